@@ -459,6 +459,94 @@ geot_status_t geot_transpose_edges(const int64_t *col, int64_t num_x_rows, const
                                    const int64_t *sorted_row, int64_t nnz, int64_t num_rows, geot_op_t op,
                                    int64_t *sorted_col_out, int64_t *row_out, float *coef_out, void *stream);
 
+/* ---- The dense half of a layer ------------------------------------------
+ * Not in the paper, whose end-to-end setting (Section V-F) leaves the update of the
+ * aggregated rows to a library's products: dropout, a gated feed-forward block with its
+ * gradients, and a product in 8-bit integers, for the rows that the reductions above
+ * make. Conventions as above, and:
+ *  - A matrix has unit stride along its columns and a row stride in elements, at least
+ *    its columns; any element-aligned address will do. Biases and scales are contiguous.
+ *  - Sums, activations and scales are held in fp32 (int32 for 8-bit products); every
+ *    output is rounded once, to nearest even, to its type.
+ *  - The temporary memory of a call is the stream's buffer up to 64 MB, else, and under
+ *    capture, stream-ordered allocations of the library's pool. All calls can be captured
+ *    in a HIP graph. Results do not depend on timing.
+ *  - Row strides, sizes, types and overlaps are checked on the host
+ *    (GEOT_ERROR_INVALID_VALUE). Zero rows or output columns are a no-op; a product over
+ *    zero input columns is zero.
+ */
+
+/* Dropout (Srivastava et al.), with a mask that is never stored:
+ *   out[r, f] = residual[r, f] + (kept(r, f) ? x[r, f] / (1 - p) : 0)
+ * residual NULL: without it. kept(r, f) is a function of (seed, offset, r, f) alone: word f mod 4 of the
+ * Philox4x32 block (7 rounds) with counter (f / 4, r, offset mod 2^32, offset / 2^32) and key seed is
+ * at least round(p * 2^32). So the gradient w.r.t. x is this call on the gradient, with the same p,
+ * seed and offset and no residual; any slice of columns that starts at 0, any type and any stride
+ * sees the same mask. A dropped element is 0 also where x is infinite or NaN. p = 0 keeps all, p = 1
+ * none. Successive calls take other offsets (or seeds); a captured call replays its own.
+ * out may be x or residual itself (same address and stride), and no other overlap. With p > 0, at most
+ * 2^32 rows of 2^34 columns. x, residual and out are of `type`.             */
+geot_status_t geot_dropout(const void *x, geot_dtype_t type, int64_t rows, int64_t F, int64_t x_stride,
+                           const void *residual, int64_t residual_stride, double p, uint64_t seed, uint64_t offset,
+                           void *out, int64_t out_stride, void *stream);
+
+/* Activations of the gated block. */
+typedef enum {
+    GEOT_ACT_SILU = 0,    /* g / (1 + exp(-g)) */
+    GEOT_ACT_GELU = 1,    /* g (1 + erf(g / sqrt 2)) / 2 */
+    GEOT_ACT_RELU = 2,
+    GEOT_ACT_SIGMOID = 3,
+    GEOT_ACT_NONE = 4     /* g */
+} geot_activation_t;
+
+/* Gated feed-forward block, both projections, the activation, the product and dropout in one pass:
+ *   g = x w_gate^T + b_gate, u = x w_up^T + b_up
+ *   out = dropout(act(g) * u; p, seed, offset)        (the mask of geot_dropout at out's elements)
+ *   x             [rows x in_features]
+ *   w_gate, w_up  [out_features x in_features], one row stride for both
+ *   b_gate, b_up  [out_features] or NULL (zero), each
+ *   out           [rows x out_features], overwritten; must not overlap an input
+ * All of `type`. g, u and their product are never written to memory (few rows over a long in_features
+ * are summed in parts: fp32 partial sums in the temporary memory).         */
+geot_status_t geot_gated_linear(const void *x, geot_dtype_t type, int64_t rows, int64_t in_features, int64_t x_stride,
+                                const void *w_gate, const void *w_up, int64_t out_features, int64_t w_stride,
+                                const void *b_gate, const void *b_up, geot_activation_t act, double p, uint64_t seed,
+                                uint64_t offset, void *out, int64_t out_stride, void *stream);
+
+/* Gradients of geot_gated_linear, from its inputs and grad_out [rows x out_features] (g and u are computed
+ * again): with d = grad_out masked and scaled as out was,
+ *   dG = d * u * act'(g), dU = d * act(g)              (relu's derivative at 0 is 0)
+ *   grad_x = dG w_gate + dU w_up   [rows x in_features]
+ *   grad_w_gate = dG^T x, grad_w_up = dU^T x   [out_features x in_features]
+ *   grad_b_gate, grad_b_up: the column sums of dG and dU   [out_features]
+ * grad_x, the two grad_w together, and each grad_b may be NULL (skipped). Outputs are contiguous, of
+ * `type`, overwritten, and overlap nothing. dG and dU are rounded to `type` between the
+ * passes (the bias gradients sum them before that). Temporary memory: dG and dU, and one copy of the weights
+ * for grad_x.                                                               */
+geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stride, const void *x, geot_dtype_t type,
+                                         int64_t rows, int64_t in_features, int64_t x_stride, const void *w_gate,
+                                         const void *w_up, int64_t out_features, int64_t w_stride, const void *b_gate,
+                                         const void *b_up, geot_activation_t act, double p, uint64_t seed, uint64_t offset,
+                                         void *grad_x, void *grad_w_gate, void *grad_w_up, void *grad_b_gate,
+                                         void *grad_b_up, void *stream);
+
+/* Rows in 8 bits, each with its scale: with a = max(2^-100, max over f of |x[r, f]|),
+ *   scale[r] = a / 127, q[r, f] = x[r, f] * (127 / a) rounded to nearest even   (-127 .. 127)
+ * so scale[r] * q[r, f] is x[r, f] to within half a step. A row with a NaN or an infinity gets scale NaN and
+ * zeros, so whatever is computed from it is NaN. Outputs overlap neither x nor each other. */
+geot_status_t geot_quantize_rows(const void *x, geot_dtype_t type, int64_t rows, int64_t F, int64_t x_stride, int8_t *q,
+                                 int64_t q_stride, float *scale, void *stream);
+
+/* Product in 8-bit integers, with a scale for each row (token) and each output channel:
+ *   out[m, n] = x_scale[m] * w_scale[n] * sum over k of xq[m, k] * wq[n, k] + bias[n]
+ *   xq [rows x in_features], wq [out_features x in_features] int8 (-128 .. 127), as geot_quantize_rows
+ *   makes them of activations and of weights; x_scale [rows], w_scale [out_features], bias [out_features]
+ *   or NULL, fp32; out of out_type, overwritten; must not overlap an input.
+ * The sums are exact (int32; in_features at most 131071).                   */
+geot_status_t geot_linear_int8(const int8_t *xq, const float *x_scale, int64_t rows, int64_t in_features, int64_t x_stride,
+                               const int8_t *wq, const float *w_scale, int64_t out_features, int64_t w_stride,
+                               const float *bias, void *out, geot_dtype_t out_type, int64_t out_stride, void *stream);
+
 /* The selector (Section III-C: a decision tree over O(1) input features,
  * compiled to if/else). Pure host function: no device access.
  *   gather  0 for geot_segment_reduce; for geot_gather_scatter 1 with edge

@@ -1,4 +1,5 @@
-"""libgeot_hip: sorted segment reduction and fused gather-weight-scatter on MI355X (gfx950).
+"""libgeot_hip: sorted segment reduction, fused gather-weight-scatter and the dense half of a layer
+(dropout, gated feed-forward block, 8-bit product) on MI355X (gfx950).
 
 The computation lives in hand-written HIP kernels behind the C-ABI of
 include/geot.h; this package only builds that library and marshals torch
@@ -27,6 +28,12 @@ from .geot import (  # noqa: F401
     gather_scatter_backward_max_arg,
     index_stats,
     transpose_edges,
+    ACTIVATIONS,
+    dropout,
+    gated_linear,
+    gated_linear_backward,
+    quantize_rows,
+    linear_int8,
     check_index,
     select,
     last_choice,

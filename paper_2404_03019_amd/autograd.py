@@ -322,3 +322,108 @@ class GINConv(torch.nn.Module):
             z = RowsLinear.apply(z, self.lin1.weight) + self.lin1.bias
         z = torch.relu(z)
         return RowsLinear.apply(z, self.lin2.weight) + self.lin2.bias
+
+
+class Dropout(torch.autograd.Function):
+    """out = residual + mask * x / (1 - p); differentiable in x and residual. The backward makes the mask
+    again from (seed, offset): nothing is kept."""
+
+    @staticmethod
+    def forward(ctx, x, p: float, seed: int, offset: int = 0, residual=None):
+        ctx.args = (p, seed, offset)
+        return geot.dropout(x, p, seed, offset, residual=residual)
+
+    @staticmethod
+    def backward(ctx, grad_out):
+        gx = None
+        if ctx.needs_input_grad[0]:
+            gx = geot.dropout(grad_out.contiguous(), *ctx.args)
+        return gx, None, None, None, grad_out if ctx.needs_input_grad[4] else None
+
+
+class GatedLinear(torch.autograd.Function):
+    """out = dropout(act(x w_gate^T + b_gate) * (x w_up^T + b_up)); differentiable in x, the weights and the
+    biases. The backward computes both projections again instead of keeping them."""
+
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, b_gate=None, b_up=None, act: str = "silu", p: float = 0.0, seed: int = 0,
+                offset: int = 0):
+        ctx.args = (act, p, seed, offset)
+        ctx.save_for_backward(x, w_gate, w_up, b_gate, b_up)
+        return geot.gated_linear(x, w_gate, w_up, b_gate, b_up, act, p, seed, offset)
+
+    @staticmethod
+    def backward(ctx, grad_out):
+        need = ctx.needs_input_grad
+        g = geot.gated_linear_backward(grad_out.contiguous(), *ctx.saved_tensors, *ctx.args, need_x=need[0],
+                                       need_w=need[1] or need[2], need_b=need[3] or need[4])
+        return (*(t if n else None for t, n in zip(g, need)), None, None, None, None)
+
+
+def dropout(x, p, seed, offset=0, residual=None):
+    """Differentiable dropout with a mask that is never stored (gradients w.r.t. x and residual)."""
+    return Dropout.apply(x, p, seed, offset, residual)
+
+
+def gated_linear(x, w_gate, w_up, b_gate=None, b_up=None, act="silu", p=0.0, seed=0, offset=0):
+    """Differentiable gated feed-forward block (gradients w.r.t. x, the weights and the biases)."""
+    return GatedLinear.apply(x, w_gate, w_up, b_gate, b_up, act, p, seed, offset)
+
+
+class Int8Linear(torch.nn.Module):
+    """y = x W^T + b with W kept in 8 bits, one scale per output channel, and x's rows quantised on the way
+    in, one scale per row. For answering only: no gradients."""
+
+    def __init__(self, linear: torch.nn.Linear):
+        super().__init__()
+        q, scale = geot.quantize_rows(linear.weight.detach())
+        self.register_buffer("weight", q)
+        self.register_buffer("scale", scale)
+        self.register_buffer("bias", linear.bias.detach().float() if linear.bias is not None else None)
+
+    def forward(self, x):
+        q, scale = geot.quantize_rows(x)
+        return geot.linear_int8(q, scale, self.weight, self.scale, self.bias, dtype=x.dtype)
+
+
+class GatedConv(torch.nn.Module):
+    """h' = h + dropout(W_down dropout(act(z W_gate^T + b_gate) * (z W_up^T + b_up))) with z the neighbours' sum,
+    mean or max: one fused gather, one fused gated block, the down projection and a fused dropout with the
+    residual. Dropout runs in training only; each call takes the next offset of the layer's seed.
+
+    `int8()` gives the layer for answering: its down projection in 8 bits."""
+
+    def __init__(self, features: int, hidden: int, reduce: str = "mean", act: str = "silu", p: float = 0.0,
+                 seed: int | None = None):
+        super().__init__()
+        self.gate = torch.nn.Linear(features, hidden)
+        self.up = torch.nn.Linear(features, hidden)
+        self.down = torch.nn.Linear(hidden, features, bias=False)
+        self.reduce, self.act, self.p = reduce, act, float(p)
+        self.seed = int(torch.randint(2 ** 62, ())) if seed is None else int(seed)
+        self.calls = 0
+
+    def int8(self):
+        """A copy of this layer that answers with its down projection in 8 bits."""
+        other = GatedConv.__new__(GatedConv)
+        torch.nn.Module.__init__(other)
+        other.gate, other.up, other.down = self.gate, self.up, Int8Linear(self.down)
+        other.reduce, other.act, other.p, other.seed, other.calls = self.reduce, self.act, 0.0, self.seed, 0
+        return other.eval()
+
+    def forward(self, h, col, row=None, num_nodes: int | None = None, weight=None):
+        """forward(h, graph) with a Graph, or forward(h, col, row, num_nodes, weight)."""
+        graph = None
+        if isinstance(col, Graph):
+            graph = col
+            col, row, num_nodes, weight = graph.col, graph.row, graph.num_nodes, graph.weight
+        if h.shape[0] != num_nodes:
+            raise ValueError("the layer adds its input: sources and destinations are the same nodes")
+        z = gather_scatter(h, col, weight, row, num_nodes, self.reduce, graph).to(h.dtype)
+        p = self.p if self.training else 0.0
+        offset = 2 * self.calls
+        if p > 0:
+            self.calls += 1
+        y = gated_linear(z, self.gate.weight, self.up.weight, self.gate.bias, self.up.bias, self.act, p, self.seed, offset)
+        y = self.down(y) if isinstance(self.down, Int8Linear) else RowsLinear.apply(y, self.down.weight)
+        return dropout(y, p, self.seed, offset + 1, residual=h)

@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "../../include/geot.h"
+#include "host.h"
 #include "internal.h"
 #include "selector_generated.h"
 
@@ -242,6 +243,9 @@ struct Workspace {
     char *p;
     size_t bytes;
 };
+
+// Temporaries of the fused gradients and the dense operators up to this size stay in the stream's buffer between calls.
+constexpr size_t kKeptBytes = (size_t)64 << 20;
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -1009,6 +1013,52 @@ geot_status_t noalloc_scratch(char **ptr) {
 }
 
 }  // namespace
+
+// ---------------------------------------------------------------------------
+// the services of host.h
+// ---------------------------------------------------------------------------
+void detail_clear() { t_detail.clear(); }
+
+geot_status_t detail_fail(geot_status_t st, const char *fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof(buf), fmt, ap);
+    va_end(ap);
+    t_detail = buf;
+    return st;
+}
+
+geot_status_t detail_hip_fail(hipError_t e, const char *what) { return hip_fail(e, what); }
+
+bool ranges_overlap(const void *a, size_t na, const void *b, size_t nb) { return overlaps(a, na, b, nb); }
+
+struct CallMemory::State {
+    Held held;
+    ScratchGuard pool;   // freed in stream order when the call ends
+};
+
+CallMemory::CallMemory(hipStream_t st) : s_(new State) { s_->pool.st = st; }
+CallMemory::~CallMemory() = default;
+
+geot_status_t CallMemory::get(size_t bytes, char **p) {
+    *p = nullptr;
+    if (bytes == 0) return GEOT_SUCCESS;
+    const hipStream_t st = s_->pool.st;
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    GEOT_HIP(hipStreamIsCapturing(st, &cap), "hipStreamIsCapturing");
+    void *mem = nullptr;
+    geot_status_t s;
+    if (bytes <= kKeptBytes && cap == hipStreamCaptureStatusNone) {
+        s = stream_scratch(bytes, st, &mem, nullptr, &s_->held);
+    } else {
+        s = scratch_alloc(&s_->pool.p, bytes, st);
+        mem = s_->pool.p;
+    }
+    *p = (char *)mem;
+    return s;
+}
+
 }  // namespace geot
 
 using namespace geot;
@@ -1306,8 +1356,6 @@ geot_status_t geot_gather_scatter_max_arg(const void *X, geot_dtype_t x_type, in
     return reduce(p, (hipStream_t)stream, choice);
 }
 
-// Temporaries of the fused gradients up to this size stay in the stream's buffer between calls.
-static constexpr size_t kKeptBytes = (size_t)64 << 20;
 
 // The fused-form gradients; for max, `given` (may be NULL) holds the recipients a forward
 // geot_gather_scatter_max_arg recorded, and then out is not read and no recipient pass runs.

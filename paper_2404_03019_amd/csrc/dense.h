@@ -1,0 +1,83 @@
+// Internal declarations of the dense operators (the update half of a layer): dropout, the gated
+// block, the 8-bit product. Not part of the public ABI (include/geot.h is).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "internal.h"
+#include "philox.h"
+
+namespace geot {
+
+constexpr int ELEM_I8 = 3;  // beside ElemType: the 8-bit product's operands
+
+enum ActFn : int { ACT_SILU = 0, ACT_GELU = 1, ACT_RELU = 2, ACT_SIGMOID = 3, ACT_NONE = 4 };
+
+// What a product's tile becomes.
+enum DenseEpi : int {
+    DENSE_GATED = 0,      // out = drop(act(g) * u)                       (two column operands)
+    DENSE_GATED_BWD = 1,  // dG, dU from the gradient of that, and their column sums (two)
+    DENSE_PLAIN = 2,      // out = the product
+    DENSE_I8 = 3,         // out = the product * sx[m] * sw[n] + bias[n]
+    DENSE_PART = 4,       // the raw sums of one part of K, to `part`
+};
+
+// C[m, n] = sum_k A[m, k] B[n, k], both operands with unit stride along k. With two column
+// operands (b1) g comes from b0 and u from b1, N columns each.
+struct DenseArgs {
+    const void *a = nullptr;
+    int64_t lda = 0;
+    const void *b0 = nullptr, *b1 = nullptr;
+    int64_t ldb = 0;
+    int64_t M = 0, N = 0, K = 0;
+    int32_t splits = 1;        // parts of K (DENSE_PART), one slab of `part` each
+    int64_t steps_per = 0;     // K steps of one part
+    int64_t tiles_m = 0, tiles_n = 0;
+    void *part = nullptr;      // [splits][M][N or 2N] fp32 (int32 for 8-bit operands)
+    const void *bias0 = nullptr, *bias1 = nullptr;  // storage type (gated), fp32 (8-bit)
+    int32_t act = 0;
+    Drop drop;
+    const void *grad = nullptr;
+    int64_t ldg = 0;
+    void *out = nullptr, *out1 = nullptr;  // DENSE_GATED_BWD: dG and dU; DENSE_PLAIN: rows from rows0 on go to out1
+    int64_t ldo = 0, rows0 = 0;
+    float *colsum = nullptr;   // DENSE_GATED_BWD: [colsum_rows][2N] partial sums over rows of dG and dU, or nullptr
+    const float *sx = nullptr, *sw = nullptr;
+    int32_t out_elem = 0;      // DENSE_I8: type of out
+};
+
+// Tile and split of a product, chosen by plan_dense from its sizes.
+struct DensePlan {
+    int big;         // 0: 128 x 128 tiles; 1: 256 x 256
+    int64_t splits;  // parts of K; more than one takes `part` and a join
+    size_t part_bytes;
+    int64_t colsum_rows;
+};
+
+DensePlan plan_dense(int elem, int epi, int64_t M, int64_t N, int64_t K, bool dual);
+// Runs the product (and the join of its parts) with `epi`; a.part holds plan.part_bytes.
+hipError_t launch_dense(int elem, int epi, DenseArgs a, const DensePlan &plan, hipStream_t st);
+#define GEOT_DENSE_LAUNCHER(NAME) \
+    hipError_t NAME(int epi, bool dual, int big, const DenseArgs &a, int64_t blocks, hipStream_t st)
+GEOT_DENSE_LAUNCHER(launch_dense_f32);
+GEOT_DENSE_LAUNCHER(launch_dense_bf16);
+GEOT_DENSE_LAUNCHER(launch_dense_f16);
+GEOT_DENSE_LAUNCHER(launch_dense_i8);
+hipError_t launch_dense_join(int elem, int epi, const DenseArgs &a, hipStream_t st);
+
+// out[c * ldo + r] = in[r * ldi + c]
+hipError_t launch_transpose2d(int elem, const void *in, int64_t ldi, int64_t rows, int64_t cols, void *out, int64_t ldo,
+                              hipStream_t st);
+// out0[n] (n < N) and out1[n - N]: sums of the rows of colsum [rows x 2N]
+hipError_t launch_colsum(int elem, const float *colsum, int64_t rows, int64_t N, float *mid, void *out0, void *out1,
+                         hipStream_t st);
+constexpr int64_t kColsumMid = 64;  // rows of `mid`, [kColsumMid x 2N]
+
+hipError_t launch_dropout(int elem, const void *x, int64_t ldx, const void *res, int64_t ldr, int64_t rows, int64_t F,
+                          const Drop &d, void *out, int64_t ldo, hipStream_t st);
+hipError_t launch_quantize_rows(int elem, const void *x, int64_t ldx, int64_t rows, int64_t F, int8_t *q, int64_t ldq,
+                                float *scale, hipStream_t st);
+
+}  // namespace geot

@@ -1,0 +1,422 @@
+// Host side of the dense operators: argument checks, the choice of tiles and splits, temporary memory
+// and the extern "C" entry points of geot.h for dropout, the gated block and the 8-bit product.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <exception>
+
+#include "../../include/geot.h"
+#include "dense.h"
+#include "host.h"
+
+namespace geot {
+namespace {
+
+constexpr int kChipCUs = 256;
+constexpr int64_t kMaxInt8K = 131071;  // (-128)(-128) K stays below 2^31
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int64_t elem_bytes(int elem) { return elem == ELEM_F32 ? 4 : elem == ELEM_I8 ? 1 : 2; }
+
+#define DENSE_TRY(expr)                             \
+    do {                                            \
+        const geot_status_t s_ = (expr);            \
+        if (s_ != GEOT_SUCCESS) return s_;          \
+    } while (0)
+#define DENSE_HIP(expr, what)                                \
+    do {                                                     \
+        const hipError_t e_ = (expr);                        \
+        if (e_ != hipSuccess) return detail_hip_fail(e_, what); \
+    } while (0)
+
+geot_status_t bad(const char *what) { return detail_fail(GEOT_ERROR_INVALID_VALUE, "%s", what); }
+
+// Nothing may be thrown out of an entry point.
+template <class F>
+geot_status_t guarded(F &&f) {
+    try {
+        detail_clear();
+        return f();
+    } catch (const std::exception &e) {
+        try {
+            return detail_fail(GEOT_ERROR_HIP, "%s", e.what());
+        } catch (...) {
+        }
+    } catch (...) {
+    }
+    return GEOT_ERROR_HIP;
+}
+
+// A matrix argument: rows x cols with row stride ld, in elements of `es` bytes.
+struct Mat {
+    const char *name;
+    const void *p;
+    int64_t rows, cols, ld, es;
+    size_t bytes() const { return p && rows > 0 && cols > 0 ? (size_t)((rows - 1) * ld + cols) * (size_t)es : 0; }
+};
+
+geot_status_t check_mat(const Mat &m) {
+    if (m.rows < 0 || m.cols < 0) return detail_fail(GEOT_ERROR_INVALID_VALUE, "%s: negative size", m.name);
+    if (m.rows == 0 || m.cols == 0) return GEOT_SUCCESS;
+    if (!m.p) return detail_fail(GEOT_ERROR_INVALID_VALUE, "%s is NULL", m.name);
+    if (((uintptr_t)m.p & (uintptr_t)(m.es - 1)) != 0)
+        return detail_fail(GEOT_ERROR_INVALID_VALUE, "%s is not aligned to its elements", m.name);
+    if (m.ld < m.cols)
+        return detail_fail(GEOT_ERROR_INVALID_VALUE, "%s: row stride %lld below its %lld columns", m.name, (long long)m.ld,
+                           (long long)m.cols);
+    if (m.ld > ((int64_t)1 << 56) / m.rows)
+        return detail_fail(GEOT_ERROR_INVALID_VALUE, "%s: size overflow", m.name);
+    return GEOT_SUCCESS;
+}
+
+// Whether `out` may share memory with `in`. A tensor written element by element from the same place of
+// another may be that tensor itself (`same`).
+geot_status_t check_apart(const Mat &out, const Mat &in, bool same = false) {
+    if (same && out.p == in.p && out.ld == in.ld) return GEOT_SUCCESS;
+    if (ranges_overlap(out.p, out.bytes(), in.p, in.bytes()))
+        return detail_fail(GEOT_ERROR_INVALID_VALUE, "%s overlaps %s", out.name, in.name);
+    return GEOT_SUCCESS;
+}
+
+geot_status_t check_type(int t) {
+    if (t != GEOT_DTYPE_F32 && t != GEOT_DTYPE_BF16 && t != GEOT_DTYPE_F16)
+        return detail_fail(GEOT_ERROR_INVALID_VALUE, "unknown storage type %d", t);
+    return GEOT_SUCCESS;
+}
+
+geot_status_t make_drop(double p, uint64_t seed, uint64_t offset, int64_t rows, int64_t cols, Drop *d) {
+    *d = Drop();
+    if (!(p >= 0.0 && p <= 1.0)) return bad("p must be in [0, 1]");
+    if (p == 0.0) return GEOT_SUCCESS;
+    if (rows > ((int64_t)1 << 32) || cols > ((int64_t)1 << 34))
+        return bad("a mask has at most 2^32 rows of 2^34 columns");
+    d->on = p == 1.0 ? 2 : 1;
+    d->threshold = (uint32_t)std::min(std::nearbyint(p * 4294967296.0), 4294967295.0);
+    d->scale = p == 1.0 ? 0.0f : (float)(1.0 / (1.0 - p));
+    d->k0 = (uint32_t)seed;
+    d->k1 = (uint32_t)(seed >> 32);
+    d->o0 = (uint32_t)offset;
+    d->o1 = (uint32_t)(offset >> 32);
+    return GEOT_SUCCESS;
+}
+
+}  // namespace
+
+DensePlan plan_dense(int elem, int epi, int64_t M, int64_t N, int64_t K, bool dual) {
+    DensePlan p{0, 1, 0, 0};
+    const int64_t steps = up(std::max<int64_t>(K, 1) * elem_bytes(elem), 128), C = dual ? 2 * N : N;
+    const int64_t t_big = up(M, 256) * up(C, 256);
+    p.big = t_big >= kChipCUs;
+    const int64_t tile = p.big ? 256 : 128;
+    const int64_t tiles = std::max<int64_t>(1, up(M, tile) * up(N, dual ? tile / 2 : tile));
+    if (epi != DENSE_GATED_BWD && tiles < kChipCUs) {
+        p.splits = std::max<int64_t>(1, std::min<int64_t>(2 * kChipCUs / tiles, steps / 4));
+        const int64_t per = up(steps, p.splits);
+        p.splits = up(steps, per);
+    }
+    if (p.splits > 1) p.part_bytes = (size_t)(p.splits * M * C) * 4;
+    p.colsum_rows = 2 * up(M, tile);
+    return p;
+}
+
+hipError_t launch_dense(int elem, int epi, DenseArgs a, const DensePlan &plan, hipStream_t st) {
+    if (a.M <= 0 || a.N <= 0) return hipSuccess;
+    const bool dual = a.b1 != nullptr;
+    const int64_t tile = plan.big ? 256 : 128, steps = up(a.K * elem_bytes(elem), 128);
+    a.tiles_m = up(a.M, tile);
+    a.tiles_n = up(a.N, dual ? tile / 2 : tile);
+    a.splits = (int32_t)plan.splits;
+    a.steps_per = up(steps, plan.splits);
+    const int64_t blocks = a.tiles_m * a.tiles_n * plan.splits;
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    const int e = plan.splits > 1 ? DENSE_PART : epi;
+    hipError_t r = hipErrorInvalidValue;
+    if (elem == ELEM_F32) r = launch_dense_f32(e, dual, plan.big, a, blocks, st);
+    else if (elem == ELEM_BF16) r = launch_dense_bf16(e, dual, plan.big, a, blocks, st);
+    else if (elem == ELEM_F16) r = launch_dense_f16(e, dual, plan.big, a, blocks, st);
+    else if (elem == ELEM_I8) r = launch_dense_i8(e, dual, plan.big, a, blocks, st);
+    if (r != hipSuccess || plan.splits == 1) return r;
+    return launch_dense_join(elem, epi, a, st);
+}
+
+namespace {
+
+// The gated block's arguments, which its two entry points share.
+struct Gated {
+    Mat x, wg, wu;
+    const void *bg, *bu;
+    int64_t M, K, N;
+    int elem;
+};
+
+geot_status_t check_gated(const Gated &q, geot_activation_t act) {
+    if ((int)act < 0 || (int)act > GEOT_ACT_NONE)
+        return detail_fail(GEOT_ERROR_INVALID_VALUE, "unknown activation %d", (int)act);
+    DENSE_TRY(check_mat(q.x));
+    DENSE_TRY(check_mat(q.wg));
+    DENSE_TRY(check_mat(q.wu));
+    if (q.M > ((int64_t)1 << 38) || q.K > INT32_MAX || q.N > INT32_MAX / 2) return bad("size overflow");
+    const uintptr_t mask = (uintptr_t)elem_bytes(q.elem) - 1;
+    if (((uintptr_t)q.bg & mask) != 0 || ((uintptr_t)q.bu & mask) != 0) return bad("a bias is not aligned to its elements");
+    return GEOT_SUCCESS;
+}
+
+
+
+geot_status_t gated_forward(const Gated &q, geot_activation_t act, const Drop &drop, const Mat &out, hipStream_t st) {
+    DenseArgs a;
+    a.a = q.x.p;
+    a.lda = q.x.ld;
+    a.b0 = q.wg.p;
+    a.b1 = q.wu.p;
+    a.ldb = q.wg.ld;
+    a.M = q.M;
+    a.N = q.N;
+    a.K = q.K;
+    a.bias0 = q.bg;
+    a.bias1 = q.bu;
+    a.act = (int)act;
+    a.drop = drop;
+    a.out = const_cast<void *>(out.p);
+    a.ldo = out.ld;
+    const DensePlan plan = plan_dense(q.elem, DENSE_GATED, q.M, q.N, q.K, true);
+    CallMemory mem(st);
+    char *part = nullptr;
+    DENSE_TRY(mem.get(plan.part_bytes, &part));
+    a.part = part;
+    DENSE_HIP(launch_dense(q.elem, DENSE_GATED, a, plan, st), "launch gated product");
+    return GEOT_SUCCESS;
+}
+
+}  // namespace
+}  // namespace geot
+
+using namespace geot;
+
+extern "C" {
+
+geot_status_t geot_dropout(const void *x, geot_dtype_t type, int64_t rows, int64_t F, int64_t x_stride,
+                           const void *residual, int64_t residual_stride, double p, uint64_t seed, uint64_t offset,
+                           void *out, int64_t out_stride, void *stream) {
+    return guarded([&]() -> geot_status_t {
+        DENSE_TRY(check_type((int)type));
+        const int64_t es = elem_bytes((int)type);
+        const Mat mx{"x", x, rows, F, x_stride, es}, mr{"residual", residual, rows, F, residual_stride, es};
+        const Mat mo{"out", out, rows, F, out_stride, es};
+        DENSE_TRY(check_mat(mx));
+        if (residual) DENSE_TRY(check_mat(mr));
+        DENSE_TRY(check_mat(mo));
+        DENSE_TRY(check_apart(mo, mx, true));
+        DENSE_TRY(check_apart(mo, mr, true));
+        Drop d;
+        DENSE_TRY(make_drop(p, seed, offset, rows, F, &d));
+        if (rows == 0 || F == 0) return GEOT_SUCCESS;
+        DENSE_HIP(launch_dropout((int)type, x, x_stride, residual, residual_stride, rows, F, d, out, out_stride,
+                                 (hipStream_t)stream),
+                  "launch dropout kernel");
+        return GEOT_SUCCESS;
+    });
+}
+
+geot_status_t geot_gated_linear(const void *x, geot_dtype_t type, int64_t rows, int64_t in_features, int64_t x_stride,
+                                const void *w_gate, const void *w_up, int64_t out_features, int64_t w_stride,
+                                const void *b_gate, const void *b_up, geot_activation_t act, double p, uint64_t seed,
+                                uint64_t offset, void *out, int64_t out_stride, void *stream) {
+    return guarded([&]() -> geot_status_t {
+        DENSE_TRY(check_type((int)type));
+        const int64_t es = elem_bytes((int)type), M = rows, K = in_features, N = out_features;
+        const Gated q{{"x", x, M, K, x_stride, es}, {"w_gate", w_gate, N, K, w_stride, es}, {"w_up", w_up, N, K, w_stride, es},
+                      b_gate, b_up, M, K, N, (int)type};
+        DENSE_TRY(check_gated(q, act));
+        const Mat mo{"out", out, M, N, out_stride, es};
+        DENSE_TRY(check_mat(mo));
+        const Mat bg{"b_gate", b_gate, 1, N, N, es}, bu{"b_up", b_up, 1, N, N, es};
+        for (const Mat &in : {q.x, q.wg, q.wu, bg, bu}) DENSE_TRY(check_apart(mo, in));
+        Drop d;
+        DENSE_TRY(make_drop(p, seed, offset, M, N, &d));
+        if (M == 0 || N == 0) return GEOT_SUCCESS;
+        return gated_forward(q, act, d, mo, (hipStream_t)stream);
+    });
+}
+
+geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stride, const void *x, geot_dtype_t type,
+                                         int64_t rows, int64_t in_features, int64_t x_stride, const void *w_gate,
+                                         const void *w_up, int64_t out_features, int64_t w_stride, const void *b_gate,
+                                         const void *b_up, geot_activation_t act, double p, uint64_t seed, uint64_t offset,
+                                         void *grad_x, void *grad_w_gate, void *grad_w_up, void *grad_b_gate,
+                                         void *grad_b_up, void *stream) {
+    return guarded([&]() -> geot_status_t {
+        DENSE_TRY(check_type((int)type));
+        const int elem = (int)type;
+        const int64_t es = elem_bytes(elem), M = rows, K = in_features, N = out_features;
+        const Gated q{{"x", x, M, K, x_stride, es}, {"w_gate", w_gate, N, K, w_stride, es}, {"w_up", w_up, N, K, w_stride, es},
+                      b_gate, b_up, M, K, N, elem};
+        DENSE_TRY(check_gated(q, act));
+        const Mat mg{"grad_out", grad_out, M, N, grad_stride, es};
+        DENSE_TRY(check_mat(mg));
+        if (!grad_w_gate != !grad_w_up) return bad("grad_w_gate and grad_w_up go together");
+        const bool need_x = grad_x, need_w = grad_w_gate, need_b = grad_b_gate || grad_b_up;
+        const Mat bg{"b_gate", b_gate, 1, N, N, es}, bu{"b_up", b_up, 1, N, N, es};
+        const Mat outs[5] = {{"grad_x", grad_x, M, K, K, es},
+                             {"grad_w_gate", grad_w_gate, N, K, K, es},
+                             {"grad_w_up", grad_w_up, N, K, K, es},
+                             {"grad_b_gate", grad_b_gate, 1, N, N, es},
+                             {"grad_b_up", grad_b_up, 1, N, N, es}};
+        for (int i = 0; i < 5; ++i) {
+            if (!outs[i].p) continue;
+            DENSE_TRY(check_mat(outs[i]));
+            for (const Mat &in : {q.x, q.wg, q.wu, bg, bu, mg}) DENSE_TRY(check_apart(outs[i], in));
+            for (int j = 0; j < i; ++j) DENSE_TRY(check_apart(outs[i], outs[j]));
+        }
+        Drop d;
+        DENSE_TRY(make_drop(p, seed, offset, M, N, &d));
+        if (!need_x && !need_w && !need_b) return GEOT_SUCCESS;
+        hipStream_t st = (hipStream_t)stream;
+
+        // dG and dU side by side, [M x 2N] in the storage type: the rounding that a framework's own
+        // gradients of the two projections would have. Every row starts on 16 bytes.
+        const int64_t lane = 16 / es, ld2 = up(2 * N, lane) * lane, ldm = up(M, lane) * lane;
+        const DensePlan p0 = plan_dense(elem, DENSE_GATED_BWD, M, N, K, true);
+        const DensePlan px = plan_dense(elem, DENSE_PLAIN, M, K, 2 * N, false);
+        const DensePlan pw = plan_dense(elem, DENSE_PLAIN, 2 * N, K, M, false);
+        size_t at = 0;
+        auto take = [&](size_t b) {
+            const size_t o = at;
+            at = (at + b + 255) & ~(size_t)255;
+            return o;
+        };
+        const size_t o_d = take((size_t)(M * ld2 * es));
+        const size_t o_cs = need_b ? take((size_t)(p0.colsum_rows * 2 * N) * 4) : 0;
+        const size_t o_mid = need_b ? take((size_t)(kColsumMid * 2 * N) * 4) : 0;
+        const size_t o_wt = need_x ? take((size_t)(K * ld2 * es)) : 0;
+        const size_t o_dt = need_w ? take((size_t)(2 * N * ldm * es)) : 0;
+        const size_t o_xt = need_w ? take((size_t)(K * ldm * es)) : 0;
+        const size_t o_part = take(std::max(need_x ? px.part_bytes : 0, need_w ? pw.part_bytes : 0));
+        CallMemory mem(st);
+        char *base = nullptr;
+        DENSE_TRY(mem.get(at, &base));
+        if (M > 0 && N > 0) {
+            DenseArgs a;
+            a.a = x;
+            a.lda = x_stride;
+            a.b0 = w_gate;
+            a.b1 = w_up;
+            a.ldb = w_stride;
+            a.M = M;
+            a.N = N;
+            a.K = K;
+            a.bias0 = b_gate;
+            a.bias1 = b_up;
+            a.act = (int)act;
+            a.drop = d;
+            a.grad = grad_out;
+            a.ldg = grad_stride;
+            a.out = base + o_d;
+            a.out1 = base + o_d + N * es;
+            a.ldo = ld2;
+            a.colsum = need_b ? (float *)(base + o_cs) : nullptr;
+            DENSE_HIP(launch_dense(elem, DENSE_GATED_BWD, a, p0, st), "launch gated gradient");
+        }
+        if (need_b && N > 0)
+            DENSE_HIP(launch_colsum(elem, (const float *)(base + o_cs), M > 0 ? p0.colsum_rows : 0, N,
+                                    (float *)(base + o_mid), grad_b_gate, grad_b_up, st),
+                      "launch bias gradient");
+        if (need_x && M > 0 && K > 0) {
+            DENSE_HIP(launch_transpose2d(elem, w_gate, w_stride, N, K, base + o_wt, ld2, st), "launch transpose");
+            DENSE_HIP(launch_transpose2d(elem, w_up, w_stride, N, K, base + o_wt + N * es, ld2, st), "launch transpose");
+            DenseArgs a;
+            a.a = base + o_d;
+            a.lda = a.ldb = ld2;
+            a.b0 = base + o_wt;
+            a.M = M;
+            a.N = K;
+            a.K = 2 * N;
+            a.out = grad_x;
+            a.ldo = K;
+            a.part = base + o_part;
+            DENSE_HIP(launch_dense(elem, DENSE_PLAIN, a, px, st), "launch input gradient");
+        }
+        if (need_w && N > 0 && K > 0) {
+            DENSE_HIP(launch_transpose2d(elem, base + o_d, ld2, M, 2 * N, base + o_dt, ldm, st), "launch transpose");
+            DENSE_HIP(launch_transpose2d(elem, x, x_stride, M, K, base + o_xt, ldm, st), "launch transpose");
+            DenseArgs a;
+            a.a = base + o_dt;
+            a.lda = a.ldb = ldm;
+            a.b0 = base + o_xt;
+            a.M = 2 * N;
+            a.N = K;
+            a.K = M;
+            a.out = grad_w_gate;
+            a.out1 = grad_w_up;
+            a.rows0 = N;
+            a.ldo = K;
+            a.part = base + o_part;
+            DENSE_HIP(launch_dense(elem, DENSE_PLAIN, a, pw, st), "launch weight gradient");
+        }
+        return GEOT_SUCCESS;
+    });
+}
+
+geot_status_t geot_quantize_rows(const void *x, geot_dtype_t type, int64_t rows, int64_t F, int64_t x_stride, int8_t *q,
+                                 int64_t q_stride, float *scale, void *stream) {
+    return guarded([&]() -> geot_status_t {
+        DENSE_TRY(check_type((int)type));
+        const Mat mx{"x", x, rows, F, x_stride, elem_bytes((int)type)}, mq{"q", q, rows, F, q_stride, 1};
+        const Mat ms{"scale", scale, 1, rows, rows, 4};
+        DENSE_TRY(check_mat(mx));
+        DENSE_TRY(check_mat(mq));
+        DENSE_TRY(check_mat(ms));
+        DENSE_TRY(check_apart(mq, mx));
+        DENSE_TRY(check_apart(ms, mx));
+        DENSE_TRY(check_apart(ms, mq));
+        if (rows == 0) return GEOT_SUCCESS;
+        DENSE_HIP(launch_quantize_rows((int)type, x, x_stride, rows, F, q, q_stride, scale, (hipStream_t)stream),
+                  "launch quantisation kernel");
+        return GEOT_SUCCESS;
+    });
+}
+
+geot_status_t geot_linear_int8(const int8_t *xq, const float *x_scale, int64_t rows, int64_t in_features, int64_t x_stride,
+                               const int8_t *wq, const float *w_scale, int64_t out_features, int64_t w_stride,
+                               const float *bias, void *out, geot_dtype_t out_type, int64_t out_stride, void *stream) {
+    return guarded([&]() -> geot_status_t {
+        DENSE_TRY(check_type((int)out_type));
+        const int64_t M = rows, K = in_features, N = out_features;
+        const Mat mx{"xq", xq, M, K, x_stride, 1}, mw{"wq", wq, N, K, w_stride, 1};
+        const Mat mo{"out", out, M, N, out_stride, elem_bytes((int)out_type)};
+        const Mat sx{"x_scale", x_scale, 1, M, M, 4}, sw{"w_scale", w_scale, 1, N, N, 4}, mb{"bias", bias, 1, N, N, 4};
+        for (const Mat &m : {mx, mw, mo, sx, sw}) DENSE_TRY(check_mat(m));
+        if (bias) DENSE_TRY(check_mat(mb));
+        if (K > kMaxInt8K) return bad("in_features above 131071: a 32-bit sum of 8-bit products could overflow");
+        if (M > ((int64_t)1 << 38) || N > INT32_MAX) return bad("size overflow");
+        for (const Mat &m : {mx, mw, sx, sw, mb}) DENSE_TRY(check_apart(mo, m));
+        if (M == 0 || N == 0) return GEOT_SUCCESS;
+        hipStream_t st = (hipStream_t)stream;
+        DenseArgs a;
+        a.a = xq;
+        a.lda = x_stride;
+        a.b0 = wq;
+        a.ldb = w_stride;
+        a.M = M;
+        a.N = N;
+        a.K = K;
+        a.sx = x_scale;
+        a.sw = w_scale;
+        a.bias0 = bias;
+        a.out = out;
+        a.out_elem = (int)out_type;
+        a.ldo = out_stride;
+        const DensePlan plan = plan_dense(ELEM_I8, DENSE_I8, M, N, K, false);
+        CallMemory mem(st);
+        char *part = nullptr;
+        DENSE_TRY(mem.get(plan.part_bytes, &part));
+        a.part = part;
+        DENSE_HIP(launch_dense(ELEM_I8, DENSE_I8, a, plan, st), "launch 8-bit product");
+        return GEOT_SUCCESS;
+    });
+}
+
+}  // extern "C"

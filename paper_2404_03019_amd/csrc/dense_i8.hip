@@ -1,0 +1,12 @@
+// Products of the dense operators, 8-bit operands with 32-bit sums.
+#include "dense_kernel.h"
+
+namespace geot {
+
+GEOT_DENSE_LAUNCHER(launch_dense_i8) {
+    if (epi == DENSE_I8) return launch_tile<ELEM_I8, DENSE_I8, false>(big, a, blocks, st);
+    if (epi == DENSE_PART) return launch_tile<ELEM_I8, DENSE_PART, false>(big, a, blocks, st);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace geot

@@ -1,0 +1,54 @@
+// The counter-based generator behind dropout: Philox4x32 (Salmon, Moraes, Dror and Shaw, "Parallel
+// random numbers: as easy as 1, 2, 3", SC 2011) with 7 rounds, the fewest that the paper reports
+// to pass every test of its statistical batteries. Element (r, f) of a mask takes word f % 4 of the
+// block with counter (f / 4, r, offset low, offset high) and key = seed, so a mask is a function
+// of (seed, offset, r, f) alone: of no stride, launch shape, type or order of the work.
+// A round is two 32 x 32 -> 64 bit products, quarter-rate instructions: 7 rounds cost about 25
+// full-rate instruction slots a word, 10 rounds 35, where reading and writing a 16-bit element at the
+// card's copy rate leaves 30.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace geot {
+
+// Dropout of one call. threshold = round(p * 2^32): an element is kept iff its word is at least that.
+struct Drop {
+    uint32_t on = 0;         // 0: no dropout; 1: by words; 2: everything is dropped (p = 1)
+    uint32_t threshold = 0;
+    float scale = 1.0f;      // 1 / (1 - p)
+    uint32_t k0 = 0, k1 = 0, o0 = 0, o1 = 0;
+};
+
+__device__ __forceinline__ uint4 philox4(uint32_t group, uint32_t row, const Drop &d) {
+    uint32_t c0 = group, c1 = row, c2 = d.o0, c3 = d.o1, k0 = d.k0, k1 = d.k1;
+#pragma unroll
+    for (int r = 0; r < 7; ++r) {
+        const uint64_t p = (uint64_t)c0 * 0xD2511F53u, q = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(q >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)q;
+        c2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)p;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return make_uint4(c0, c1, c2, c3);
+}
+
+// v[0..3], elements (row, 4 * group ..), become scale * v where kept and 0 where dropped (also
+// where v is not finite).
+__device__ __forceinline__ void drop4(float *v, uint32_t group, uint32_t row, const Drop &d) {
+    if (d.on == 2) {
+        v[0] = v[1] = v[2] = v[3] = 0.0f;
+        return;
+    }
+    const uint4 w = philox4(group, row, d);
+    v[0] = w.x >= d.threshold ? v[0] * d.scale : 0.0f;
+    v[1] = w.y >= d.threshold ? v[1] * d.scale : 0.0f;
+    v[2] = w.z >= d.threshold ? v[2] * d.scale : 0.0f;
+    v[3] = w.w >= d.threshold ? v[3] * d.scale : 0.0f;
+}
+
+}  // namespace geot

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libgeot_hip.so")
 
 OPS = {"sum": 0, "mean": 1, "max": 2}
 FAMILIES = {"auto": 0, "ep": 1, "sp": 2}
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3, "none": 4}
 STATUS = {0: "success", 1: "invalid value", 2: "index not sorted", 3: "index out of range",
           4: "HIP runtime error", 5: "unsupported kernel choice"}
 
@@ -93,6 +94,13 @@ def lib() -> ctypes.CDLL:
     L.geot_segment_reduce_noalloc.argtypes = [p, p, i64, i64, i64, ctypes.c_int, p, p]
     L.geot_noalloc_scratch_bytes.argtypes = []
     L.geot_noalloc_scratch_bytes.restype = sz
+    u64, dbl = ctypes.c_uint64, ctypes.c_double
+    L.geot_dropout.argtypes = [p, ctypes.c_int, i64, i64, i64, p, i64, dbl, u64, u64, p, i64, p]
+    gated = [p, ctypes.c_int, i64, i64, i64, p, p, i64, i64, p, p, ctypes.c_int, dbl, u64, u64]
+    L.geot_gated_linear.argtypes = [*gated, p, i64, p]
+    L.geot_gated_linear_backward.argtypes = [p, i64, *gated, p, p, p, p, p, p]
+    L.geot_quantize_rows.argtypes = [p, ctypes.c_int, i64, i64, i64, p, i64, p, p]
+    L.geot_linear_int8.argtypes = [p, p, i64, i64, i64, p, p, i64, i64, p, p, ctypes.c_int, i64, p]
     L.geot_last_choice.argtypes = [pc]
     L.geot_release_scratch.argtypes = []
     L.geot_profile_begin.argtypes = [i32]
@@ -107,7 +115,9 @@ def lib() -> ctypes.CDLL:
                  "geot_last_choice", "geot_profile_begin", "geot_profile_end", "geot_release_scratch",
                  "geot_segment_reduce_backward", "geot_gather_scatter_backward",
                  "geot_segment_reduce_workspace_size", "geot_gather_scatter_workspace_size",
-                 "geot_segment_reduce_ws", "geot_gather_scatter_ws", "geot_segment_reduce_noalloc"):
+                 "geot_segment_reduce_ws", "geot_gather_scatter_ws", "geot_segment_reduce_noalloc",
+                 "geot_dropout", "geot_gated_linear", "geot_gated_linear_backward", "geot_quantize_rows",
+                 "geot_linear_int8"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -600,6 +610,187 @@ def transpose_edges(col: torch.Tensor, weight: torch.Tensor | None, row: torch.T
                                         _stream(row.device))
     _raise(st)
     return sc, rt, cf
+
+
+def _rows(t: torch.Tensor, name: str, dtype) -> int:
+    """Checks the type and layout of a matrix argument whose rows may be apart (unit stride along the
+    columns); its row stride in elements."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+        raise TypeError(f"{name} must be {dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have 2 dimensions")
+    r, c = t.shape
+    if c > 1 and r > 0 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit stride along its columns")
+    if r <= 1 or c == 0:
+        return max(c, 1)
+    if t.stride(0) < c:
+        raise ValueError(f"{name} must have rows that do not overlap")
+    return t.stride(0)
+
+
+def _ptr(t: torch.Tensor | None):
+    return t.data_ptr() if t is not None else None
+
+
+def _mask_args(p, seed, offset):
+    p = float(p)
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p must be in [0, 1]")
+    return p, int(seed) & (2 ** 64 - 1), int(offset) & (2 ** 64 - 1)
+
+
+def dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual: torch.Tensor | None = None,
+            out: torch.Tensor | None = None) -> torch.Tensor:
+    """out = residual + mask * x / (1 - p), the mask a function of (seed, offset, row, column) that is
+    never stored (geot_dropout).
+
+    x is [rows, F] (rows may be apart) or one-dimensional (one row, e.g. edge weights), fp32, bf16 or fp16;
+    residual and out are like it. The gradient w.r.t. x is dropout(grad, p, seed, offset)."""
+    if isinstance(x, torch.Tensor) and x.dim() == 1:
+        r2 = residual[None] if residual is not None and residual.dim() == 1 else residual
+        o2 = out[None] if out is not None and out.dim() == 1 else out
+        y = dropout(x[None], p, seed, offset, r2, o2)
+        return out if out is not None else y[0]
+    ld = _rows(x, "x", tuple(DTYPES))
+    p, seed, offset = _mask_args(p, seed, offset)
+    R, F = x.shape
+    ldr = ldo = F
+    if residual is not None:
+        ldr = _rows(residual, "residual", x.dtype)
+        _shape(residual, "residual", (R, F))
+    if out is not None:
+        ldo = _rows(out, "out", x.dtype)
+        _shape(out, "out", (R, F))
+    _on_gpu(x=x, residual=residual, out=out)
+    if out is None:
+        out = torch.empty((R, F), dtype=x.dtype, device=x.device)
+    with _OnDevice(x.device):
+        st = lib().geot_dropout(x.data_ptr(), DTYPES[x.dtype], R, F, ld, _ptr(residual), ldr, p, seed, offset,
+                                out.data_ptr(), ldo, _stream(x.device))
+    _raise(st)
+    return out
+
+
+def _gated_args(x, w_gate, w_up, b_gate, b_up, act, p, seed, offset):
+    """The arguments that the gated block's forward and gradients share, checked: (x's row stride, the
+    weights' row stride, (p, seed, offset))."""
+    ld = _rows(x, "x", tuple(DTYPES))
+    ldw = _rows(w_gate, "w_gate", x.dtype)
+    ldu = _rows(w_up, "w_up", x.dtype)
+    N, K = w_gate.shape
+    _shape(w_up, "w_up", (N, K))
+    if x.shape[1] != K:
+        raise ValueError(f"x must have the weights' {K} columns, got {x.shape[1]}")
+    if ldw != ldu:
+        raise ValueError("w_gate and w_up must have the same row stride")
+    for name, b in (("b_gate", b_gate), ("b_up", b_up)):
+        if b is not None:
+            _dev(b, name, x.dtype, 1)
+            _shape(b, name, (N,))
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
+    return ld, ldw, _mask_args(p, seed, offset)
+
+
+def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: torch.Tensor | None = None,
+                 b_up: torch.Tensor | None = None, act: str = "silu", p: float = 0.0, seed: int = 0, offset: int = 0,
+                 out: torch.Tensor | None = None) -> torch.Tensor:
+    """out = dropout(act(x w_gate^T + b_gate) * (x w_up^T + b_up)) in one pass (geot_gated_linear).
+
+    x [rows, K], the weights [N, K], the biases [N], all of one type: fp32, bf16 or fp16 (sums in fp32).
+    act: silu, gelu, relu, sigmoid or none; p, seed and offset as in dropout."""
+    ld, ldw, (p, seed, offset) = _gated_args(x, w_gate, w_up, b_gate, b_up, act, p, seed, offset)
+    M, (N, K) = x.shape[0], w_gate.shape
+    ldo = N
+    if out is not None:
+        ldo = _rows(out, "out", x.dtype)
+        _shape(out, "out", (M, N))
+    _on_gpu(x=x, w_gate=w_gate, w_up=w_up, b_gate=b_gate, b_up=b_up, out=out)
+    if out is None:
+        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    with _OnDevice(x.device):
+        st = lib().geot_gated_linear(x.data_ptr(), DTYPES[x.dtype], M, K, ld, w_gate.data_ptr(), w_up.data_ptr(), N,
+                                     ldw, _ptr(b_gate), _ptr(b_up), ACTIVATIONS[act], p, seed, offset, out.data_ptr(),
+                                     ldo, _stream(x.device))
+    _raise(st)
+    return out
+
+
+def gated_linear_backward(grad_out: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
+                          b_gate: torch.Tensor | None = None, b_up: torch.Tensor | None = None, act: str = "silu",
+                          p: float = 0.0, seed: int = 0, offset: int = 0, need_x: bool = True, need_w: bool = True,
+                          need_b: bool = True):
+    """(grad_x, grad_w_gate, grad_w_up, grad_b_gate, grad_b_up) of gated_linear, of the inputs' type
+    (geot_gated_linear_backward); None where not needed, and for a bias that is None."""
+    ld, ldw, (p, seed, offset) = _gated_args(x, w_gate, w_up, b_gate, b_up, act, p, seed, offset)
+    M, (N, K) = x.shape[0], w_gate.shape
+    ldg = _rows(grad_out, "grad_out", x.dtype)
+    _shape(grad_out, "grad_out", (M, N))
+    _on_gpu(grad_out=grad_out, x=x, w_gate=w_gate, w_up=w_up, b_gate=b_gate, b_up=b_up)
+
+    def empty(need, *shape):
+        return torch.empty(shape, dtype=x.dtype, device=x.device) if need else None
+
+    gx, gwg, gwu = empty(need_x, M, K), empty(need_w, N, K), empty(need_w, N, K)
+    gbg, gbu = empty(need_b and b_gate is not None, N), empty(need_b and b_up is not None, N)
+    with _OnDevice(x.device):
+        st = lib().geot_gated_linear_backward(grad_out.data_ptr(), ldg, x.data_ptr(), DTYPES[x.dtype], M, K, ld,
+                                              w_gate.data_ptr(), w_up.data_ptr(), N, ldw, _ptr(b_gate), _ptr(b_up),
+                                              ACTIVATIONS[act], p, seed, offset, _ptr(gx), _ptr(gwg), _ptr(gwu),
+                                              _ptr(gbg), _ptr(gbu), _stream(x.device))
+    _raise(st)
+    return gx, gwg, gwu, gbg, gbu
+
+
+def quantize_rows(x: torch.Tensor):
+    """(q, scale): the rows of x in 8 bits, scale[r] * q[r] = x[r] to half a step (geot_quantize_rows).
+
+    x [rows, F] fp32, bf16 or fp16; q int8 [rows, F], scale fp32 [rows]. A row that holds NaN or an infinity
+    gets scale NaN."""
+    ld = _rows(x, "x", tuple(DTYPES))
+    _on_gpu(x=x)
+    R, F = x.shape
+    q = torch.empty((R, F), dtype=torch.int8, device=x.device)
+    scale = torch.empty(R, dtype=torch.float32, device=x.device)
+    with _OnDevice(x.device):
+        st = lib().geot_quantize_rows(x.data_ptr(), DTYPES[x.dtype], R, F, ld, q.data_ptr(), max(F, 1), scale.data_ptr(),
+                                      _stream(x.device))
+    _raise(st)
+    return q, scale
+
+
+def linear_int8(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor,
+                bias: torch.Tensor | None = None, dtype: torch.dtype = torch.bfloat16,
+                out: torch.Tensor | None = None) -> torch.Tensor:
+    """out = x_scale[:, None] * w_scale * (xq wq^T) + bias, exact 8-bit products (geot_linear_int8).
+
+    xq [rows, K] and wq [N, K] int8 with scales [rows] and [N] (quantize_rows of the activations and of
+    the weights), bias [N] fp32; out of `dtype` (fp32, bf16, fp16)."""
+    ldx, ldw = _rows(xq, "xq", torch.int8), _rows(wq, "wq", torch.int8)
+    M, K = xq.shape
+    N = wq.shape[0]
+    _shape(wq, "wq", (N, K))
+    for name, t, n in (("x_scale", x_scale, M), ("w_scale", w_scale, N), ("bias", bias, N)):
+        if t is not None or name != "bias":
+            _dev(t, name, torch.float32, 1)
+            _shape(t, name, (n,))
+    if dtype not in DTYPES:
+        raise TypeError(f"dtype must be one of {tuple(DTYPES)}")
+    ldo = N
+    if out is not None:
+        ldo = _rows(out, "out", dtype)
+        _shape(out, "out", (M, N))
+    _on_gpu(xq=xq, x_scale=x_scale, wq=wq, w_scale=w_scale, bias=bias, out=out)
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=xq.device)
+    with _OnDevice(xq.device):
+        st = lib().geot_linear_int8(xq.data_ptr(), x_scale.data_ptr(), M, K, ldx, wq.data_ptr(), w_scale.data_ptr(), N,
+                                    ldw, _ptr(bias), out.data_ptr(), DTYPES[dtype], ldo, _stream(xq.device))
+    _raise(st)
+    return out
 
 
 def index_stats(index: torch.Tensor, num_segments: int) -> dict:

@@ -24,13 +24,23 @@ enum DenseEpi : int {
     DENSE_PART = 4,       // the raw sums of one part of K, to `part`
 };
 
-// C[m, n] = sum_k A[m, k] B[n, k], both operands with unit stride along k. With two column
-// operands (b1) g comes from b0 and u from b1, N columns each.
+// How a product's operands lie in memory: k along their rows, or a row per k.
+enum DenseMode : int {
+    DENSE_NT = 0,  // k along the rows of both
+    DENSE_NN = 1,  // along A's; B has a row per k
+    DENSE_TN = 2,  // both have a row per k
+};
+
+enum DenseTile : int { DENSE_TILE_128 = 0, DENSE_TILE_256 = 1 };
+
+// C[m, n] = sum_k A[m, k] B[n, k]. With DENSE_NT and b1 there are two column operands: g comes from b0 and u
+// from b1, N columns each. With DENSE_NN and b1 K comes twice: A's second K columns start seg_a bytes
+// after the first, and go with b1.
 struct DenseArgs {
     const void *a = nullptr;
     int64_t lda = 0;
     const void *b0 = nullptr, *b1 = nullptr;
-    int64_t ldb = 0;
+    int64_t ldb = 0, seg_a = 0;
     int64_t M = 0, N = 0, K = 0;
     int32_t splits = 1;        // parts of K (DENSE_PART), one slab of `part` each
     int64_t steps_per = 0;     // K steps of one part
@@ -41,8 +51,9 @@ struct DenseArgs {
     Drop drop;
     const void *grad = nullptr;
     int64_t ldg = 0;
-    void *out = nullptr, *out1 = nullptr;  // DENSE_GATED_BWD: dG and dU; DENSE_PLAIN: rows from rows0 on go to out1
-    int64_t ldo = 0, rows0 = 0;
+    // DENSE_GATED_BWD: dG and dU; DENSE_PLAIN: with out1, rows 0 .. rows1 go to out, rows0 .. rows0 + rows1 there
+    void *out = nullptr, *out1 = nullptr;
+    int64_t ldo = 0, rows0 = 0, rows1 = 0;
     float *colsum = nullptr;   // DENSE_GATED_BWD: [colsum_rows][2N] partial sums over rows of dG and dU, or nullptr
     const float *sx = nullptr, *sw = nullptr;
     int32_t out_elem = 0;      // DENSE_I8: type of out
@@ -50,26 +61,27 @@ struct DenseArgs {
 
 // Tile and split of a product, chosen by plan_dense from its sizes.
 struct DensePlan {
-    int big;         // 0: 128 x 128 tiles; 1: 256 x 256
-    int64_t splits;  // parts of K; more than one takes `part` and a join
+    int tile;         // DenseTile
+    bool direct;      // whole steps are loaded straight into LDS
+    int64_t splits;   // parts of K; more than one takes `part` and a join
+    int64_t steps_per;
+    int64_t tiles_m, tiles_n;
     size_t part_bytes;
     int64_t colsum_rows;
 };
 
-DensePlan plan_dense(int elem, int epi, int64_t M, int64_t N, int64_t K, bool dual);
+// dual: two column operands (DENSE_NT); segments: of K (DENSE_NN)
+DensePlan plan_dense(int elem, int epi, int64_t M, int64_t N, int64_t K, bool dual, int segments, bool direct);
 // Runs the product (and the join of its parts) with `epi`; a.part holds plan.part_bytes.
-hipError_t launch_dense(int elem, int epi, DenseArgs a, const DensePlan &plan, hipStream_t st);
+hipError_t launch_dense(int elem, int epi, int mode, DenseArgs a, const DensePlan &plan, hipStream_t st);
 #define GEOT_DENSE_LAUNCHER(NAME) \
-    hipError_t NAME(int epi, bool dual, int big, const DenseArgs &a, int64_t blocks, hipStream_t st)
+    hipError_t NAME(int epi, int mode, int tile, bool direct, const DenseArgs &a, int64_t blocks, hipStream_t st)
 GEOT_DENSE_LAUNCHER(launch_dense_f32);
 GEOT_DENSE_LAUNCHER(launch_dense_bf16);
 GEOT_DENSE_LAUNCHER(launch_dense_f16);
 GEOT_DENSE_LAUNCHER(launch_dense_i8);
 hipError_t launch_dense_join(int elem, int epi, const DenseArgs &a, hipStream_t st);
 
-// out[c * ldo + r] = in[r * ldi + c]
-hipError_t launch_transpose2d(int elem, const void *in, int64_t ldi, int64_t rows, int64_t cols, void *out, int64_t ldo,
-                              hipStream_t st);
 // out0[n] (n < N) and out1[n - N]: sums of the rows of colsum [rows x 2N]
 hipError_t launch_colsum(int elem, const float *colsum, int64_t rows, int64_t N, float *mid, void *out0, void *out1,
                          hipStream_t st);

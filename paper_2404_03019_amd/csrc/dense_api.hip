@@ -105,39 +105,47 @@ geot_status_t make_drop(double p, uint64_t seed, uint64_t offset, int64_t rows, 
 
 }  // namespace
 
-DensePlan plan_dense(int elem, int epi, int64_t M, int64_t N, int64_t K, bool dual) {
-    DensePlan p{0, 1, 0, 0};
-    const int64_t steps = up(std::max<int64_t>(K, 1) * elem_bytes(elem), 128), C = dual ? 2 * N : N;
+// Whether every whole step of an operand can be loaded straight into LDS: 16-byte chunks at 16-byte
+// addresses, at offsets of 32 bits from the tile's first element; with a row per k (`cols` of them) chunks
+// wholly inside or outside the columns.
+static bool direct_ok(const void *p, int64_t ld, int64_t es, int64_t cols = 0) {
+    return ((uintptr_t)p & 15) == 0 && ld * es % 16 == 0 && ld * es < ((int64_t)1 << 23) && cols * es % 16 == 0;
+}
+
+DensePlan plan_dense(int elem, int epi, int64_t M, int64_t N, int64_t K, bool dual, int segments, bool direct) {
+    DensePlan p{DENSE_TILE_128, direct, 1, 0, 0, 0, 0, 0};
+    const int64_t steps = K * elem_bytes(elem) / 128 * segments, C = dual ? 2 * N : N;   // whole steps
     const int64_t t_big = up(M, 256) * up(C, 256);
-    p.big = t_big >= kChipCUs;
-    const int64_t tile = p.big ? 256 : 128;
-    const int64_t tiles = std::max<int64_t>(1, up(M, tile) * up(N, dual ? tile / 2 : tile));
-    if (epi != DENSE_GATED_BWD && tiles < kChipCUs) {
-        p.splits = std::max<int64_t>(1, std::min<int64_t>(2 * kChipCUs / tiles, steps / 4));
-        const int64_t per = up(steps, p.splits);
-        p.splits = up(steps, per);
+    if (direct && t_big >= kChipCUs) p.tile = DENSE_TILE_256;
+    const int64_t tile = p.tile == DENSE_TILE_256 ? 256 : 128;
+    p.tiles_m = up(M, tile);
+    p.tiles_n = up(N, dual ? tile / 2 : tile);
+    const int64_t tiles = std::max<int64_t>(1, p.tiles_m * p.tiles_n);
+    p.steps_per = std::max<int64_t>(steps, 1);
+    if (epi != DENSE_GATED_BWD && tiles < kChipCUs && steps > 1) {
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2 * kChipCUs / tiles, steps / 4));
+        p.steps_per = up(up(steps, want), 2) * 2;   // even: the kernel takes steps in pairs
+        p.splits = up(steps, p.steps_per);
     }
     if (p.splits > 1) p.part_bytes = (size_t)(p.splits * M * C) * 4;
-    p.colsum_rows = 2 * up(M, tile);
+    p.colsum_rows = 2 * p.tiles_m;
     return p;
 }
 
-hipError_t launch_dense(int elem, int epi, DenseArgs a, const DensePlan &plan, hipStream_t st) {
+hipError_t launch_dense(int elem, int epi, int mode, DenseArgs a, const DensePlan &plan, hipStream_t st) {
     if (a.M <= 0 || a.N <= 0) return hipSuccess;
-    const bool dual = a.b1 != nullptr;
-    const int64_t tile = plan.big ? 256 : 128, steps = up(a.K * elem_bytes(elem), 128);
-    a.tiles_m = up(a.M, tile);
-    a.tiles_n = up(a.N, dual ? tile / 2 : tile);
+    a.tiles_m = plan.tiles_m;
+    a.tiles_n = plan.tiles_n;
     a.splits = (int32_t)plan.splits;
-    a.steps_per = up(steps, plan.splits);
+    a.steps_per = plan.steps_per;
     const int64_t blocks = a.tiles_m * a.tiles_n * plan.splits;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const int e = plan.splits > 1 ? DENSE_PART : epi;
     hipError_t r = hipErrorInvalidValue;
-    if (elem == ELEM_F32) r = launch_dense_f32(e, dual, plan.big, a, blocks, st);
-    else if (elem == ELEM_BF16) r = launch_dense_bf16(e, dual, plan.big, a, blocks, st);
-    else if (elem == ELEM_F16) r = launch_dense_f16(e, dual, plan.big, a, blocks, st);
-    else if (elem == ELEM_I8) r = launch_dense_i8(e, dual, plan.big, a, blocks, st);
+    if (elem == ELEM_F32) r = launch_dense_f32(e, mode, plan.tile, plan.direct, a, blocks, st);
+    else if (elem == ELEM_BF16) r = launch_dense_bf16(e, mode, plan.tile, plan.direct, a, blocks, st);
+    else if (elem == ELEM_F16) r = launch_dense_f16(e, mode, plan.tile, plan.direct, a, blocks, st);
+    else if (elem == ELEM_I8) r = launch_dense_i8(e, mode, plan.tile, plan.direct, a, blocks, st);
     if (r != hipSuccess || plan.splits == 1) return r;
     return launch_dense_join(elem, epi, a, st);
 }
@@ -166,6 +174,10 @@ geot_status_t check_gated(const Gated &q, geot_activation_t act) {
 
 
 
+bool gated_direct(const Gated &q) {
+    return direct_ok(q.x.p, q.x.ld, q.x.es) && direct_ok(q.wg.p, q.wg.ld, q.x.es) && direct_ok(q.wu.p, q.wu.ld, q.x.es);
+}
+
 geot_status_t gated_forward(const Gated &q, geot_activation_t act, const Drop &drop, const Mat &out, hipStream_t st) {
     DenseArgs a;
     a.a = q.x.p;
@@ -182,12 +194,12 @@ geot_status_t gated_forward(const Gated &q, geot_activation_t act, const Drop &d
     a.drop = drop;
     a.out = const_cast<void *>(out.p);
     a.ldo = out.ld;
-    const DensePlan plan = plan_dense(q.elem, DENSE_GATED, q.M, q.N, q.K, true);
+    const DensePlan plan = plan_dense(q.elem, DENSE_GATED, q.M, q.N, q.K, true, 1, gated_direct(q));
     CallMemory mem(st);
     char *part = nullptr;
     DENSE_TRY(mem.get(plan.part_bytes, &part));
     a.part = part;
-    DENSE_HIP(launch_dense(q.elem, DENSE_GATED, a, plan, st), "launch gated product");
+    DENSE_HIP(launch_dense(q.elem, DENSE_GATED, DENSE_NT, a, plan, st), "launch gated product");
     return GEOT_SUCCESS;
 }
 
@@ -276,12 +288,14 @@ geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stri
         if (!need_x && !need_w && !need_b) return GEOT_SUCCESS;
         hipStream_t st = (hipStream_t)stream;
 
-        // dG and dU side by side, [M x 2N] in the storage type: the rounding that a framework's own
-        // gradients of the two projections would have. Every row starts on 16 bytes.
-        const int64_t lane = 16 / es, ld2 = up(2 * N, lane) * lane, ldm = up(M, lane) * lane;
-        const DensePlan p0 = plan_dense(elem, DENSE_GATED_BWD, M, N, K, true);
-        const DensePlan px = plan_dense(elem, DENSE_PLAIN, M, K, 2 * N, false);
-        const DensePlan pw = plan_dense(elem, DENSE_PLAIN, 2 * N, K, M, false);
+        // dG and dU side by side in the storage type, [M x Np] each: the rounding that the gradients of two
+        // separate projections would have. Each starts on 16 bytes in every row.
+        const int64_t lane = 16 / es, Np = up(N, lane) * lane, ld2 = 2 * Np;
+        const DensePlan p0 = plan_dense(elem, DENSE_GATED_BWD, M, N, K, true, 1, gated_direct(q));
+        const DensePlan px = plan_dense(elem, DENSE_PLAIN, M, K, N, false, 2,
+                                        direct_ok(w_gate, w_stride, es, K) && direct_ok(w_up, w_stride, es, K) && ld2 * es < ((int64_t)1 << 23));
+        const DensePlan pw = plan_dense(elem, DENSE_PLAIN, ld2, K, M, false, 1,
+                                        direct_ok(x, x_stride, es, K) && ld2 * es < ((int64_t)1 << 23));
         size_t at = 0;
         auto take = [&](size_t b) {
             const size_t o = at;
@@ -291,9 +305,6 @@ geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stri
         const size_t o_d = take((size_t)(M * ld2 * es));
         const size_t o_cs = need_b ? take((size_t)(p0.colsum_rows * 2 * N) * 4) : 0;
         const size_t o_mid = need_b ? take((size_t)(kColsumMid * 2 * N) * 4) : 0;
-        const size_t o_wt = need_x ? take((size_t)(K * ld2 * es)) : 0;
-        const size_t o_dt = need_w ? take((size_t)(2 * N * ldm * es)) : 0;
-        const size_t o_xt = need_w ? take((size_t)(K * ldm * es)) : 0;
         const size_t o_part = take(std::max(need_x ? px.part_bytes : 0, need_w ? pw.part_bytes : 0));
         CallMemory mem(st);
         char *base = nullptr;
@@ -315,46 +326,47 @@ geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stri
             a.grad = grad_out;
             a.ldg = grad_stride;
             a.out = base + o_d;
-            a.out1 = base + o_d + N * es;
+            a.out1 = base + o_d + Np * es;
             a.ldo = ld2;
             a.colsum = need_b ? (float *)(base + o_cs) : nullptr;
-            DENSE_HIP(launch_dense(elem, DENSE_GATED_BWD, a, p0, st), "launch gated gradient");
+            DENSE_HIP(launch_dense(elem, DENSE_GATED_BWD, DENSE_NT, a, p0, st), "launch gated gradient");
         }
         if (need_b && N > 0)
             DENSE_HIP(launch_colsum(elem, (const float *)(base + o_cs), M > 0 ? p0.colsum_rows : 0, N,
                                     (float *)(base + o_mid), grad_b_gate, grad_b_up, st),
                       "launch bias gradient");
-        if (need_x && M > 0 && K > 0) {
-            DENSE_HIP(launch_transpose2d(elem, w_gate, w_stride, N, K, base + o_wt, ld2, st), "launch transpose");
-            DENSE_HIP(launch_transpose2d(elem, w_up, w_stride, N, K, base + o_wt + N * es, ld2, st), "launch transpose");
+        if (need_x) {   // dG w_gate + dU w_up: K in two segments
             DenseArgs a;
             a.a = base + o_d;
-            a.lda = a.ldb = ld2;
-            a.b0 = base + o_wt;
+            a.lda = ld2;
+            a.seg_a = Np * es;
+            a.b0 = w_gate;
+            a.b1 = w_up;
+            a.ldb = w_stride;
             a.M = M;
             a.N = K;
-            a.K = 2 * N;
+            a.K = N;
             a.out = grad_x;
             a.ldo = K;
             a.part = base + o_part;
-            DENSE_HIP(launch_dense(elem, DENSE_PLAIN, a, px, st), "launch input gradient");
+            DENSE_HIP(launch_dense(elem, DENSE_PLAIN, DENSE_NN, a, px, st), "launch input gradient");
         }
-        if (need_w && N > 0 && K > 0) {
-            DENSE_HIP(launch_transpose2d(elem, base + o_d, ld2, M, 2 * N, base + o_dt, ldm, st), "launch transpose");
-            DENSE_HIP(launch_transpose2d(elem, x, x_stride, M, K, base + o_xt, ldm, st), "launch transpose");
+        if (need_w) {   // [dG dU]^T x; the rows between dG's and dU's are padding
             DenseArgs a;
-            a.a = base + o_dt;
-            a.lda = a.ldb = ldm;
-            a.b0 = base + o_xt;
-            a.M = 2 * N;
+            a.a = base + o_d;
+            a.lda = ld2;
+            a.b0 = x;
+            a.ldb = x_stride;
+            a.M = ld2;
             a.N = K;
             a.K = M;
             a.out = grad_w_gate;
             a.out1 = grad_w_up;
-            a.rows0 = N;
+            a.rows0 = Np;
+            a.rows1 = N;
             a.ldo = K;
             a.part = base + o_part;
-            DENSE_HIP(launch_dense(elem, DENSE_PLAIN, a, pw, st), "launch weight gradient");
+            DENSE_HIP(launch_dense(elem, DENSE_PLAIN, DENSE_TN, a, pw, st), "launch weight gradient");
         }
         return GEOT_SUCCESS;
     });
@@ -409,12 +421,12 @@ geot_status_t geot_linear_int8(const int8_t *xq, const float *x_scale, int64_t r
         a.out = out;
         a.out_elem = (int)out_type;
         a.ldo = out_stride;
-        const DensePlan plan = plan_dense(ELEM_I8, DENSE_I8, M, N, K, false);
+        const DensePlan plan = plan_dense(ELEM_I8, DENSE_I8, M, N, K, false, 1, direct_ok(xq, x_stride, 1) && direct_ok(wq, w_stride, 1));
         CallMemory mem(st);
         char *part = nullptr;
         DENSE_TRY(mem.get(plan.part_bytes, &part));
         a.part = part;
-        DENSE_HIP(launch_dense(ELEM_I8, DENSE_I8, a, plan, st), "launch 8-bit product");
+        DENSE_HIP(launch_dense(ELEM_I8, DENSE_I8, DENSE_NT, a, plan, st), "launch 8-bit product");
         return GEOT_SUCCESS;
     });
 }

@@ -3,6 +3,6 @@
 
 namespace geot {
 
-GEOT_DENSE_LAUNCHER(launch_dense_bf16) { return launch_float<ELEM_BF16>(epi, dual, big, a, blocks, st); }
+GEOT_DENSE_LAUNCHER(launch_dense_bf16) { return launch_float<ELEM_BF16>(epi, mode, tile, direct, a, blocks, st); }
 
 }  // namespace geot

@@ -4,8 +4,9 @@
 namespace geot {
 
 GEOT_DENSE_LAUNCHER(launch_dense_i8) {
-    if (epi == DENSE_I8) return launch_tile<ELEM_I8, DENSE_I8, false>(big, a, blocks, st);
-    if (epi == DENSE_PART) return launch_tile<ELEM_I8, DENSE_PART, false>(big, a, blocks, st);
+    if (mode != DENSE_NT) return hipErrorInvalidValue;
+    if (epi == DENSE_I8) return launch_tile<ELEM_I8, DENSE_I8, false, DENSE_NT>(tile, direct, a, blocks, st);
+    if (epi == DENSE_PART) return launch_tile<ELEM_I8, DENSE_PART, false, DENSE_NT>(tile, direct, a, blocks, st);
     return hipErrorInvalidValue;
 }
 

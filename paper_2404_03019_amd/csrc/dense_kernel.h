@@ -1,22 +1,32 @@
 // The matrix products of the dense operators on gfx950's matrix instructions.
 //
-// C[m, n] = sum_k A[m, k] B[n, k]: rows m are graph nodes (tokens), columns n output channels. A block
-// takes a BM x BN tile and walks K in steps of 128 bytes of a row (64 16-bit, 32 fp32 or 128 8-bit
-// elements), so one layout serves every type: a tile of R rows is R x 128 bytes in LDS, each row eight
-// 16-byte chunks, and a lane's operand of a 16 x 16 matrix instruction is one chunk of its row (k in the
-// order of the chunks, the same for both operands, so the order inside K does not matter).
+// C[m, n] = sum_k A[m, k] B[n, k]: rows m are graph nodes (tokens) and columns n output channels; in the
+// gradients m or n is a feature and k a channel or a node. A block takes a BM x BN tile and walks K in
+// steps of 128 bytes (64 16-bit, 32 fp32 or 128 8-bit elements), so one layout serves every type. An operand
+// lies in memory either with k along its rows () or with a row per k:
+//   rows of k:  a tile of R rows is R x 128 bytes in LDS. A lane's operand of a 16 x 16 matrix instruction is
+//               one 16-byte chunk of its row (k in the order of the chunks, the same for both operands, so
+//               the order inside K does not matter).
+//   row per k:  64 (fp32: 32) rows of R elements. The transposing LDS read gives a lane four k of its
+//               column; fp32, which has none, takes four loads of one column.
+// Either way 16-byte chunks change places inside a row of LDS by an XOR with a key of the row, so that lanes
+// that read in one cycle find different banks, and a tile's chunks stand in LDS in the order of the
+// threads, which lets them be loaded into LDS directly (16 bytes a lane, no registers).
 //
-// The weights are the instruction's row operand: its result then holds, in one lane, consecutive output
-// columns of one row m. Weight rows are dealt to the fragments so that a lane's fragments together hold
-// 4 * PF consecutive columns (n = 4 * PF * (lane / 16) + 4 f + i), one wide store a row.
+// The columns' operand is the instruction's row operand: its result then holds, in one lane, columns next to
+// each other of one row m. With k along rows the columns are dealt to the fragments so that a lane's
+// fragments together hold 4 * PF consecutive columns (n = 4 * PF * (lane / 16) + 4 f + i), one wide store a
+// row; with a row per k a lane has four at a time.
 //
-// Chunks are exchanged inside their row by an XOR with a key of the row that differs between any eight
-// lanes that read one bank group in one cycle.
+// Two LDS buffers: while a step is multiplied the next one is on its way. Steps that K cuts short come first,
+// through registers, with zeros for what is not there; a step of zeros makes their number even, so that the
+// loop goes over whole pairs and its sums stay where they are.
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "common.h"
 #include "dense.h"
@@ -29,9 +39,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t half_t __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
 // 16 bytes at any address of the element's alignment (global memory takes any alignment in one load)
 typedef uint32_t chunk_any __attribute__((ext_vector_type(4), aligned(1)));
 typedef uint32_t chunk_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_void;
 
 constexpr int kStepBytes = 128;
 
@@ -66,209 +80,410 @@ __device__ __forceinline__ typename AccOf<E>::type mma(chunk_t w, chunk_t x, typ
     }
 }
 
-// 16 bytes at p, of which the row holds `left` (from p; any number); bytes beyond are 0 and not read
+// The same with the sums pinned to accumulation registers, for tiles whose sums fill all 256 of them: the
+// compiler moves such sums between the two register files on every turn of the loop otherwise. An MFMA that
+// reads a register which a vector instruction has just written needs two wait states, which the compiler
+// does not know to insert here; behind another MFMA (16 cycles) they cost nothing.
 template <int E>
-__device__ __forceinline__ chunk_t load_chunk(const char *p, int64_t left) {
-    if (left >= 16) return *reinterpret_cast<const chunk_any *>(p);
-    constexpr int ES = E == ELEM_F32 ? 4 : E == ELEM_I8 ? 1 : 2;
-    chunk_t v = {0, 0, 0, 0};
+__device__ __forceinline__ void mma_pinned(chunk_t w, chunk_t x, typename AccOf<E>::type &acc) {
+    if constexpr (E == ELEM_BF16) {
+        asm("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
+    } else if constexpr (E == ELEM_F16) {
+        asm("s_nop 1\n\tv_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
+    } else if constexpr (E == ELEM_I8) {
+        asm("s_nop 1\n\tv_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
+    } else {
+        const f32x4 a = __builtin_bit_cast(f32x4, w), b = __builtin_bit_cast(f32x4, x);
 #pragma unroll
+        for (int j = 0; j < 4; ++j) asm("s_nop 1\n\tv_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(acc) : "v"(a[j]), "v"(b[j]));
+    }
+}
+// between the last of these and the first other use of the sums: the wait states of the longest MFMA
+template <class Acc>
+__device__ __forceinline__ void settle(Acc &acc) {
+    asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc));
+}
+
+// 16 bytes at p, of which `left` may be read (any number); bytes beyond are 0. What is read ends a run of at
+// least 16 readable bytes, unless `narrow`: a chunk cut short is the run's last 16 bytes, shifted.
+template <int ES>
+__device__ __forceinline__ chunk_t load_chunk(const char *p, int64_t left, bool narrow) {
+    chunk_t v = {0, 0, 0, 0};
+    if (left >= 16) return *reinterpret_cast<const chunk_any *>(p);
+    if (left <= 0) return v;
+    if (!narrow) {
+        const int cut = 16 - (int)left;   // 1 .. 15 bytes
+        const chunk_t w = *reinterpret_cast<const chunk_any *>(p - cut);
+        const uint64_t lo = (uint64_t)w.y << 32 | w.x, hi = (uint64_t)w.w << 32 | w.z;
+        const int bits = 8 * (cut & 7);
+        const uint64_t carry = bits ? hi << (64 - bits) : 0;
+        const uint64_t a = cut >= 8 ? hi >> bits : lo >> bits | carry, b = cut >= 8 ? 0 : hi >> bits;
+        return chunk_t{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+    }
     for (int i = 0; i < 16 / ES; ++i) {
-        if (i * ES < left) {
-            uint32_t x;
-            if constexpr (ES == 4) x = reinterpret_cast<const uint32_t *>(p)[i];
-            else if constexpr (ES == 2) x = reinterpret_cast<const uint16_t *>(p)[i];
-            else x = reinterpret_cast<const uint8_t *>(p)[i];
-            v[i * ES / 4] |= x << (i * ES % 4 * 8);
-        }
+        if (i * ES >= left) break;
+        uint32_t x;
+        if constexpr (ES == 4) x = reinterpret_cast<const uint32_t *>(p)[i];
+        else if constexpr (ES == 2) x = reinterpret_cast<const uint16_t *>(p)[i];
+        else x = reinterpret_cast<const uint8_t *>(p)[i];
+        x <<= i * ES % 4 * 8;
+        const int at = i * ES / 4;
+        v.x |= at == 0 ? x : 0;
+        v.y |= at == 1 ? x : 0;
+        v.z |= at == 2 ? x : 0;
+        v.w |= at == 3 ? x : 0;
     }
     return v;
 }
 
-template <int E, int BM, int BN, int WM, int WN, int EPI, bool DUAL>
-__global__ void __launch_bounds__(WM * WN * 64) dense_kernel(const DenseArgs a) {
+// One operand's tile of R rows (columns): how its chunks lie in LDS and where they come from. Chunk i
+// (of R * 8) stands at 16 i.
+template <int E, int R, bool KMAJOR, int NV>
+struct Tile {
+    static constexpr int ES = E == ELEM_F32 ? 4 : E == ELEM_I8 ? 1 : 2;
+    static constexpr int KS = kStepBytes / ES;              // k of one step
+    static constexpr bool kRowPerK = KMAJOR;
+    static constexpr int ROW = KMAJOR ? R * ES : kStepBytes;  // bytes of one row of LDS
+    static constexpr int CPR = ROW / 16;
+
+    // NV: rows are read by lanes in steps of NV after every fourth (the dealt columns); 0: one after another
+    static __device__ __forceinline__ int key(int row) {
+        if constexpr (!KMAJOR) {
+            if constexpr (NV > 4) return (row & 3) | (((row / NV) & 1) << 2);
+            else return row & 7;
+        } else if constexpr (ES == 2) {
+            return (row & 3) << 1;
+        } else {
+            return ((row >> 2) & 1) << 2;
+        }
+    }
+    // chunk i: its row of LDS, and the chunk of that row in memory that it holds
+    static __device__ __forceinline__ int row_of(int i) { return i / CPR; }
+    static __device__ __forceinline__ int chunk_of(int i) { return (i % CPR) ^ key(i / CPR); }
+
+    // fragment: the operand of one matrix instruction for 16 rows (columns) from `first`, half kk of the
+    // step. With dealt columns `first` already holds the lane's own row.
+    static __device__ __forceinline__ chunk_t fragment(const char *lds, int row, int kk, int r16, int c4) {
+        if constexpr (!KMAJOR) {
+            return *reinterpret_cast<const chunk_t *>(lds + row * kStepBytes + (((4 * kk + c4) ^ key(row)) << 4));
+        } else if constexpr (ES == 2) {
+            const int k = 32 * kk + 8 * c4 + (r16 >> 2), at = (row + 4 * (r16 & 3)) * 2;
+            typedef __attribute__((address_space(3))) i16x4 lds4;
+            const int p = k * ROW + (((at >> 4) ^ key(k)) << 4) + (at & 15);   // rows k and k + 4 have one key
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(lds + p));
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(lds + p + 4 * ROW));
+            chunk_t v;
+            v.xy = __builtin_bit_cast(half_t, lo);
+            v.zw = __builtin_bit_cast(half_t, hi);
+            return v;
+        } else {
+            chunk_t v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = 16 * kk + 4 * c4 + j, at = (row + r16) * 4;
+                v[j] = *reinterpret_cast<const uint32_t *>(lds + k * ROW + (((at >> 4) ^ key(k)) << 4) + (at & 15));
+            }
+            return v;
+        }
+    }
+};
+
+// DENSE_NT: k along the rows of both operands. DENSE_NN: along A's, a row per k for B; K may come in two
+// segments with their own bases. DENSE_TN: a row per k for both.
+template <int E, int BM, int BN, int WM, int WN, int EPI, bool DUAL, int MODE, bool DIRECT>
+__global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) dense_kernel(const DenseArgs a) {
     constexpr int T = WM * WN * 64;
     constexpr int ES = E == ELEM_F32 ? 4 : E == ELEM_I8 ? 1 : 2;
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
-    constexpr int PF = DUAL ? FN / 2 : FN;          // fragments of one column operand
-    constexpr int NV = 4 * PF;                      // consecutive columns of one lane
-    constexpr int CA = BM * 8 / T, CB = BN * 8 / T; // chunks a thread stages
-    constexpr int HB = DUAL ? BN / 2 : BN;          // columns of one operand in the tile
+    constexpr int PF = DUAL ? FN / 2 : FN;            // fragments of one column operand
+    constexpr int CA = BM * 8 / T, CB = BN * 8 / T;   // chunks a thread stages
+    constexpr int HB = DUAL ? BN / 2 : BN;            // columns of one operand in the tile
+    constexpr bool KA = MODE == DENSE_TN, KB = MODE != DENSE_NT;
+    typedef Tile<E, BM, KA, 0> TA;
+    typedef Tile<E, BN, KB, KB ? 0 : 4 * PF> TB;
     typedef typename AccOf<E>::type Acc;
-    __shared__ __align__(16) char lds[2][(BM + BN) * kStepBytes];
+    static_assert(!DUAL || MODE == DENSE_NT, "two column operands have k along their rows");
+    __shared__ __align__(16) char lds0[(BM + BN) * kStepBytes];
+    __shared__ __align__(16) char lds1[(BM + BN) * kStepBytes];
 
     // Blocks go round the chiplets in turn: give each chiplet a run of neighbouring tiles, so that what
     // they share stays in its L2.
-    const int64_t nb = gridDim.x, b = blockIdx.x, x8 = b & 7, q8 = nb >> 3, r8 = nb & 7;
-    const int64_t id = x8 * q8 + (x8 < r8 ? x8 : r8) + (b >> 3);
-    const int64_t tiles = a.tiles_m * a.tiles_n;
-    const int64_t split = id / tiles, t = id - split * tiles;
+    const uint32_t nb = gridDim.x, b = blockIdx.x, x8 = b & 7, q8 = nb >> 3, r8 = nb & 7;
+    const uint32_t id = x8 * q8 + (x8 < r8 ? x8 : r8) + (b >> 3);
+    const uint32_t tiles_m = (uint32_t)a.tiles_m, tiles_n = (uint32_t)a.tiles_n, tiles = tiles_m * tiles_n;
+    const uint32_t split = id / tiles, t = id - split * tiles;
     // tiles in groups of 8 rows of tiles
-    const int64_t per = 8 * a.tiles_n, grp = t / per, gm = a.tiles_m - grp * 8 < 8 ? a.tiles_m - grp * 8 : 8;
-    const int64_t tm = grp * 8 + (t - grp * per) % gm, tn = (t - grp * per) / gm;
-    const int64_t m0 = tm * BM, n0 = tn * HB;
+    const uint32_t per = 8 * tiles_n, grp = t / per, gm = tiles_m - grp * 8 < 8 ? tiles_m - grp * 8 : 8;
+    const uint32_t in = t - grp * per, tn = in / gm, tm = grp * 8 + (in - tn * gm);
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * HB;
 
-    const int64_t kbytes = a.K * ES;
-    const int64_t all = (kbytes + kStepBytes - 1) / kStepBytes;
-    const int64_t s0 = split * a.steps_per, s1 = s0 + a.steps_per < all ? s0 + a.steps_per : all;
+    // Steps of K. This split's whole ones are [s0, s1), of each segment in turn (DENSE_NN: two); the first
+    // split also takes the step that ends each segment short. The host gives every split but the last an even
+    // number, so with two segments all of them, and no more than two steps are `odd` (short, or zeros).
+    const int segs = MODE == DENSE_NN && a.b1 ? 2 : 1;
+    const int64_t whole = a.K / TA::KS, all_whole = whole * segs;
+    const int64_t s0 = split * a.steps_per, s1 = s0 + a.steps_per < all_whole ? s0 + a.steps_per : all_whole;
+    const int shorts = split == 0 && whole * TA::KS < a.K ? segs : 0;
+    const int64_t mine = (s1 > s0 ? s1 - s0 : 0) + shorts;
+    const int odd = mine == 0 ? 2 : shorts + (int)(mine & 1);
+    const int64_t slots = mine == 0 ? 2 : mine + (mine & 1);   // slot j: odd step j, then whole step s0 + j - odd
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int wm = wave % WM, wn = wave / WM;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave % WM, wn = wave / WM, r16 = lane & 15, c4 = lane >> 4;
 
-    // staging: thread's chunk c of row (tid + c T) / 8. Rows beyond the end read the last row; what
-    // they give is never stored.
-    const char *pa[CA], *pb[CB];
-    int la[CA], lb[CB];
-    const int chunk = tid & 7;
+    // Where a thread's chunks come from, relative to the tile's (and step's) first element. Rows and
+    // columns beyond the end read others in their place; what they give is never stored.
+    const int64_t lda = a.lda * ES, ldb = a.ldb * ES;
+    const int64_t mleft = a.M - m0, nleft = a.N - n0;   // rows (columns) of the tile that exist: at least 1
+    auto place = [&](auto tile, int i, int64_t left, int64_t *row, int *byte, int fold) {
+        typedef decltype(tile) TT;
+        const int r = TT::row_of(i), c = TT::chunk_of(i) * 16;
+        if constexpr (TT::kRowPerK) {
+            *row = r;
+            *byte = c < left * ES ? c : 0;
+        } else {
+            const int rr = r % fold;   // both column operands' rows start at the tile's first column
+            *row = rr < left ? rr : left - 1;
+            *byte = c;
+        }
+    };
+    // direct loads: 32-bit offsets (the host has checked that they fit)
+    uint32_t oa[CA], ob[CB];
+    if constexpr (DIRECT) {
 #pragma unroll
-    for (int c = 0; c < CA; ++c) {
-        const int row = (tid + c * T) >> 3;
-        const int64_t m = m0 + row < a.M ? m0 + row : a.M - 1;
-        pa[c] = (const char *)a.a + m * a.lda * ES + chunk * 16;
-        la[c] = row * kStepBytes + ((chunk ^ (row & 7)) << 4);
-    }
+        for (int c = 0; c < CA; ++c) {
+            int64_t row;
+            int byte;
+            place(TA{}, tid + c * T, mleft, &row, &byte, BM);
+            oa[c] = (uint32_t)(row * lda) + byte;
+        }
 #pragma unroll
-    for (int c = 0; c < CB; ++c) {
-        const int row = (tid + c * T) >> 3, col = DUAL ? row % HB : row;
-        const int64_t n = n0 + col < a.N ? n0 + col : a.N - 1;
-        const void *base = DUAL && row >= HB ? a.b1 : a.b0;
-        pb[c] = (const char *)base + n * a.ldb * ES + chunk * 16;
-        const int key = (row & 3) | (((row / NV) & 1) << 2);
-        lb[c] = (BM + row) * kStepBytes + ((chunk ^ key) << 4);
+        for (int c = 0; c < CB; ++c) {
+            int64_t row;
+            int byte;
+            place(TB{}, tid + c * T, nleft, &row, &byte, HB);
+            ob[c] = (uint32_t)(row * ldb) + byte;
+        }
     }
+    const char *const basea = (const char *)a.a + (KA ? m0 * ES : m0 * lda);
+    const char *const baseb = (const char *)a.b0 + (KB ? n0 * ES : n0 * ldb);
+    const char *const baseb1 = a.b1 ? (const char *)a.b1 + (KB ? n0 * ES : n0 * ldb) : nullptr;
+    const int64_t inca = KA ? TA::KS * lda : kStepBytes, incb = KB ? TB::KS * ldb : kStepBytes;
 
+    const bool narrow_a = (KA ? a.M : a.K) * ES < 16, narrow_b = (KB ? a.N : a.K) * ES < 16;
+    struct Source {
+        const char *a, *b, *b1;
+    };
+    auto source = [&](bool second, int64_t sk) -> Source {
+        return Source{basea + (second ? a.seg_a : 0) + sk * inca, (second ? baseb1 : baseb) + sk * incb,
+                      DUAL ? baseb1 + sk * incb : nullptr};
+    };
+    // Chunk c of the step from `p`, through registers. kleft: how many k there are in the step.
+    auto chunk_a = [&](const Source &p, int c, int64_t kleft) -> chunk_t {
+        int64_t row;
+        int byte;
+        place(TA{}, tid + c * T, mleft, &row, &byte, BM);
+        const int64_t left = KA ? (row < kleft ? mleft * ES - byte : 0) : kleft * ES - byte;
+        return load_chunk<ES>(p.a + row * lda + byte, left, narrow_a);
+    };
+    auto chunk_b = [&](const Source &p, int c, int64_t kleft) -> chunk_t {
+        int64_t row;
+        int byte;
+        place(TB{}, tid + c * T, nleft, &row, &byte, HB);
+        const int64_t left = KB ? (row < kleft ? nleft * ES - byte : 0) : kleft * ES - byte;
+        return load_chunk<ES>((DUAL && c * T >= HB * 8 ? p.b1 : p.b) + row * ldb + byte, left, narrow_b);
+    };
+    // a whole step: straight into LDS, or into registers and from there
+    chunk_t ra[DIRECT ? 1 : CA], rb[DIRECT ? 1 : CB];
+    auto issue = [&](char *lds, int64_t slot) {
+        const int64_t s = s0 + slot - odd;
+        const bool second = MODE == DENSE_NN && s >= whole;
+        const Source p = source(second, second ? s - whole : s);
+        if constexpr (DIRECT) {
+#pragma unroll
+            for (int c = 0; c < CA; ++c)
+                __builtin_amdgcn_global_load_lds((global_void *)(p.a + oa[c]), (lds_void *)(lds + (c * T + wave * 64) * 16),
+                                                 16, 0, 0);
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+                __builtin_amdgcn_global_load_lds((global_void *)((DUAL && c * T >= HB * 8 ? p.b1 : p.b) + ob[c]),
+                                                 (lds_void *)(lds + BM * kStepBytes + (c * T + wave * 64) * 16), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int c = 0; c < CA; ++c) ra[c] = chunk_a(p, c, TA::KS);
+#pragma unroll
+            for (int c = 0; c < CB; ++c) rb[c] = chunk_b(p, c, TA::KS);
+        }
+    };
+    auto land = [&](char *lds) {
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int c = 0; c < CA; ++c) *reinterpret_cast<chunk_t *>(lds + (tid + c * T) * 16) = ra[c];
+#pragma unroll
+            for (int c = 0; c < CB; ++c) *reinterpret_cast<chunk_t *>(lds + BM * kStepBytes + (tid + c * T) * 16) = rb[c];
+        }
+    };
+    static_assert(!DUAL || HB * 8 % T == 0, "a thread's chunk is of one column operand");
+
+    // the lane's row of A and columns of B in LDS
+    const int arow = wm * (BM / WM) + (KA ? 0 : r16);
+    int brow[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int f = j % PF;
+        brow[j] = (j / PF) * HB + wn * (16 * PF) + (KB ? 16 * f : 4 * PF * (r16 >> 2) + 4 * f + (r16 & 3));
+    }
     Acc acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
 
-    chunk_t ra[CA], rb[CB];
-    auto fetch = [&](int64_t s) {
-        const int64_t at = s * kStepBytes, left = kbytes - at - chunk * 16;
-        if (at + kStepBytes <= kbytes) {
+    struct Frags {
+        chunk_t x[FM], w[FN];
+    };
+    constexpr int kAccRegs = FM * FN * 4;
+    constexpr bool PINNED = kAccRegs >= 256;
+    auto read_w = [&](Frags &f, const char *lds, int kk, int j) {
+        f.w[j] = TB::fragment(lds + BM * kStepBytes, brow[j], kk, r16, c4);
+    };
+    auto read_x = [&](Frags &f, const char *lds, int kk, int i) {
+        f.x[i] = TA::fragment(lds, arow + 16 * i, kk, r16, c4);
+    };
+    auto multiply = [&](const Frags &f, int i) {
 #pragma unroll
-            for (int c = 0; c < CA; ++c) ra[c] = *reinterpret_cast<const chunk_any *>(pa[c] + at);
-#pragma unroll
-            for (int c = 0; c < CB; ++c) rb[c] = *reinterpret_cast<const chunk_any *>(pb[c] + at);
-        } else {
-#pragma unroll
-            for (int c = 0; c < CA; ++c) ra[c] = load_chunk<E>(pa[c] + at, left);
-#pragma unroll
-            for (int c = 0; c < CB; ++c) rb[c] = load_chunk<E>(pb[c] + at, left);
+        for (int j = 0; j < FN; ++j) {
+            if constexpr (PINNED) mma_pinned<E>(f.w[j], f.x[i], acc[i][j]);
+            else acc[i][j] = mma<E>(f.w[j], f.x[i], acc[i][j]);
         }
     };
-    auto put = [&](int buf) {
-#pragma unroll
-        for (int c = 0; c < CA; ++c) *reinterpret_cast<chunk_t *>(&lds[buf][la[c]]) = ra[c];
-#pragma unroll
-        for (int c = 0; c < CB; ++c) *reinterpret_cast<chunk_t *>(&lds[buf][lb[c]]) = rb[c];
-    };
-
-    // fragment addresses: row of the tile and its key; the chunk is (4 kk + lane / 16) ^ key
-    const int r16 = lane & 15, c4 = lane >> 4;
-    const int arow = wm * (BM / WM) + r16, akey = arow & 7;
-    int brow[FN], bkey[FN];
-#pragma unroll
-    for (int j = 0; j < FN; ++j) {
-        const int f = j % PF;
-        const int row = (j / PF) * HB + wn * (16 * PF) + NV * (r16 >> 2) + 4 * f + (r16 & 3);
-        brow[j] = (BM + row) * kStepBytes;
-        bkey[j] = (row & 3) | (((row / NV) & 1) << 2);
-    }
-
-    if (s0 < s1) {
-        fetch(s0);
-        put(0);
-    }
-    __syncthreads();
-    for (int64_t s = s0; s < s1; ++s) {
-        const int buf = (int)(s - s0) & 1;
-        if (s + 1 < s1) fetch(s + 1);
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            chunk_t fa[FM], fb[FN];
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-                fb[j] = *reinterpret_cast<const chunk_t *>(&lds[buf][brow[j] + (((4 * kk + c4) ^ bkey[j]) << 4)]);
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-                fa[i] = *reinterpret_cast<const chunk_t *>(
-                    &lds[buf][(arow + 16 * i) * kStepBytes + (((4 * kk + c4) ^ akey) << 4)]);
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = mma<E>(fb[j], fa[i], acc[i][j]);
-        }
-        if (s + 1 < s1) put(buf ^ 1);
+    // Between two turns no wave writes what another reads: before one, every load into LDS has landed
+    // (vmcnt 0 counts them) and every read of the buffer that is written next is done.
+    auto turn = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0f70);
         __syncthreads();
+    };
+    // an odd step, through registers: what a segment has beyond its whole steps, or nothing
+    auto issue_odd = [&](char *lds, int64_t slot) {
+        const Source p = source(MODE == DENSE_NN && slot == 1, whole);
+        const int64_t kleft = slot < shorts ? a.K - whole * TA::KS : 0;
+        chunk_t r[CA > CB ? CA : CB];
+#pragma unroll
+        for (int c = 0; c < CA; ++c) r[c] = chunk_a(p, c, kleft);
+#pragma unroll
+        for (int c = 0; c < CA; ++c) *reinterpret_cast<chunk_t *>(lds + (tid + c * T) * 16) = r[c];
+#pragma unroll
+        for (int c = 0; c < CB; ++c) r[c] = chunk_b(p, c, kleft);
+#pragma unroll
+        for (int c = 0; c < CB; ++c) *reinterpret_cast<chunk_t *>(lds + BM * kStepBytes + (tid + c * T) * 16) = r[c];
+    };
+#pragma unroll 1
+    for (int j = 0; j < 2; ++j) {
+        char *lds = j ? lds1 : lds0;
+        if (j < odd) {
+            issue_odd(lds, j);
+        } else {
+            issue(lds, j);
+            land(lds);
+        }
+    }
+    if constexpr (PINNED) {
+        // One wave a SIMD: the next half's operands are read while this one's are multiplied, in this order:
+        // those that the next half needs first come first.
+        Frags f0, f1;
+        auto phase = [&](const Frags &now, Frags &next, const char *lds, int kk) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+#pragma unroll
+                for (int r = i * (FN + FM) / FM; r < (i + 1) * (FN + FM) / FM; ++r) {
+                    if (r < FN) read_w(next, lds, kk, r);
+                    else read_x(next, lds, kk, r - FN);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(now, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        turn();
+#pragma unroll
+        for (int j = 0; j < FN; ++j) read_w(f0, lds0, 0, j);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) read_x(f0, lds0, 0, i);
+        for (int64_t j = 2;; j += 2) {
+            phase(f0, f1, lds0, 1);
+            turn();
+            const bool more = j < slots;
+            if (more) issue(lds0, j);
+            phase(f1, f0, lds1, 0);
+            phase(f0, f1, lds1, 1);
+            turn();
+            if (more) issue(lds1, j + 1);
+            phase(f1, f0, lds0, 0);   // after the last pair what is read here is not used
+            if (!more) break;
+        }
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) settle(acc[i][j]);
+    } else {
+        Frags f;
+        auto product = [&](const char *lds) {
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j) read_w(f, lds, kk, j);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) read_x(f, lds, kk, i);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) multiply(f, i);
+            }
+        };
+        turn();
+        for (int64_t j = 2;; j += 2) {
+            product(lds0);
+            turn();
+            const bool more = j < slots;
+            if (more) issue(lds0, j);
+            product(lds1);
+            if (!more) break;
+            land(lds0);
+            turn();
+            issue(lds1, j + 1);
+            land(lds1);
+        }
     }
 
-    // epilogue: this lane has columns n .. n + NV of rows m + 16 i
-    const int64_t n = n0 + wn * (16 * PF) + NV * c4;
-    const int64_t mrow = m0 + wm * (BM / WM) + r16;
-    float csg[NV], csu[NV];
-    if constexpr (EPI == DENSE_GATED_BWD) {
-#pragma unroll
-        for (int v = 0; v < NV; ++v) csg[v] = csu[v] = 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int64_t m = mrow + 16 * i;
-        if (m < a.M && n < a.N) {
-            typename AccOf<E>::scalar g[NV], u[NV];
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                g[v] = acc[i][v / 4][v % 4];
-                if constexpr (DUAL) u[v] = acc[i][PF + v / 4][v % 4];
-            }
-            finish<E, EPI, NV, DUAL>(a, split, m, n, g, u);
-            if constexpr (EPI == DENSE_GATED_BWD) {
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    csg[v] += g[v];
-                    csu[v] += u[v];
-                }
-            }
-        }
-    }
-    if constexpr (EPI == DENSE_GATED_BWD) {
-        if (a.colsum) {
-            float *dst = a.colsum + (tm * WM + wm) * 2 * a.N;
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-#pragma unroll
-                for (int o = 1; o < 16; o <<= 1) {
-                    csg[v] += __shfl_xor(csg[v], o);
-                    csu[v] += __shfl_xor(csu[v], o);
-                }
-                if (r16 == 0 && n + v < a.N) {
-                    dst[n + v] = csg[v];
-                    dst[a.N + n + v] = csu[v];
-                }
-            }
-        }
-    }
+    epilogue<E, EPI, FM, FN, PF, DUAL, KB ? 4 : 4 * PF>(a, split, m0 + wm * (BM / WM) + r16,
+                                                        n0 + wn * (16 * PF) + (KB ? 4 : 4 * PF) * c4, acc,
+                                                        (int64_t)tm * WM + wm, r16);
 }
 
-template <int E, int EPI, bool DUAL>
-hipError_t launch_tile(int big, const DenseArgs &a, int64_t blocks, hipStream_t st) {
-    if (big)
-        hipLaunchKernelGGL((dense_kernel<E, 256, 256, 2, 4, EPI, DUAL>), dim3((unsigned)blocks), dim3(512), 0, st, a);
+template <int E, int EPI, bool DUAL, int MODE>
+hipError_t launch_tile(int tile, bool direct, const DenseArgs &a, int64_t blocks, hipStream_t st) {
+    const dim3 grid((unsigned)blocks);
+    if (tile == DENSE_TILE_256)
+        hipLaunchKernelGGL((dense_kernel<E, 256, 256, 2, 2, EPI, DUAL, MODE, true>), grid, dim3(256), 0, st, a);
+    else if (direct)
+        hipLaunchKernelGGL((dense_kernel<E, 128, 128, 2, 2, EPI, DUAL, MODE, true>), grid, dim3(256), 0, st, a);
     else
-        hipLaunchKernelGGL((dense_kernel<E, 128, 128, 2, 2, EPI, DUAL>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((dense_kernel<E, 128, 128, 2, 2, EPI, DUAL, MODE, false>), grid, dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
 template <int E>
-hipError_t launch_float(int epi, bool dual, int big, const DenseArgs &a, int64_t blocks, hipStream_t st) {
-    switch (epi) {
-        case DENSE_GATED: return launch_tile<E, DENSE_GATED, true>(big, a, blocks, st);
-        case DENSE_GATED_BWD: return launch_tile<E, DENSE_GATED_BWD, true>(big, a, blocks, st);
-        case DENSE_PLAIN: return launch_tile<E, DENSE_PLAIN, false>(big, a, blocks, st);
-        case DENSE_PART:
-            return dual ? launch_tile<E, DENSE_PART, true>(big, a, blocks, st)
-                        : launch_tile<E, DENSE_PART, false>(big, a, blocks, st);
+hipError_t launch_float(int epi, int mode, int tile, bool direct, const DenseArgs &a, int64_t blocks, hipStream_t st) {
+    if (mode == DENSE_NT) {
+        switch (epi) {
+            case DENSE_GATED: return launch_tile<E, DENSE_GATED, true, DENSE_NT>(tile, direct, a, blocks, st);
+            case DENSE_GATED_BWD: return launch_tile<E, DENSE_GATED_BWD, true, DENSE_NT>(tile, direct, a, blocks, st);
+            case DENSE_PART: return launch_tile<E, DENSE_PART, true, DENSE_NT>(tile, direct, a, blocks, st);
+        }
+    } else if (mode == DENSE_NN) {
+        if (epi == DENSE_PLAIN) return launch_tile<E, DENSE_PLAIN, false, DENSE_NN>(tile, direct, a, blocks, st);
+        if (epi == DENSE_PART) return launch_tile<E, DENSE_PART, false, DENSE_NN>(tile, direct, a, blocks, st);
+    } else {
+        if (epi == DENSE_PLAIN) return launch_tile<E, DENSE_PLAIN, false, DENSE_TN>(tile, direct, a, blocks, st);
+        if (epi == DENSE_PART) return launch_tile<E, DENSE_PART, false, DENSE_TN>(tile, direct, a, blocks, st);
     }
     return hipErrorInvalidValue;
 }

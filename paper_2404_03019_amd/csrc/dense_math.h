@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "dense.h"
 
@@ -77,111 +78,186 @@ __device__ __forceinline__ float sigmoid(float g) {
     else return __builtin_amdgcn_rcpf(1.0f + __expf(-g));
 }
 
-// the activation, and its derivative in *d
-template <int E>
-__device__ __forceinline__ float activate(int act, float g, float *d) {
-    switch (act) {
-        case ACT_SILU: {
-            const float s = sigmoid<E>(g);
-            *d = s * (1.0f + g * (1.0f - s));
-            return g * s;
+// The activation, and its derivative in *d.
+// GELU's distribution function is erfc(-g / sqrt 2) / 2. For 16-bit results erfc is formula 7.1.26 of
+// Abramowitz and Stegun, Handbook of Mathematical Functions (a polynomial in 1 / (1 + 0.3275911 x) times
+// exp(-x^2), within 1.5e-7), whose exponential the derivative needs anyway.
+template <int E, int ACT>
+__device__ __forceinline__ float activate(float g, float *d) {
+    if constexpr (ACT == ACT_SILU) {
+        const float s = sigmoid<E>(g);
+        *d = s * (1.0f + g * (1.0f - s));
+        return g * s;
+    } else if constexpr (ACT == ACT_GELU) {
+        float c, e;
+        if constexpr (E == ELEM_F32) {
+            c = 0.5f * (1.0f + erff(g * 0.70710678f));
+            e = expf(-0.5f * g * g);
+        } else {
+            const float x = fabsf(g) * 0.70710678f, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
+            e = __expf(-0.5f * g * g);
+            const float q = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f +
+                            t * 1.061405429f)))) * e * 0.5f;
+            c = g < 0.0f ? q : 1.0f - q;
         }
-        case ACT_GELU: {
-            const float c = 0.5f * (1.0f + erff(g * 0.70710678f));
-            const float e = E == ELEM_F32 ? expf(-0.5f * g * g) : __expf(-0.5f * g * g);
-            *d = c + g * e * 0.39894228f;
-            return g * c;
-        }
-        case ACT_RELU:
-            *d = g > 0.0f ? 1.0f : 0.0f;
-            return g > 0.0f ? g : (g != g ? g : 0.0f);
-        case ACT_SIGMOID: {
-            const float s = sigmoid<E>(g);
-            *d = s * (1.0f - s);
-            return s;
-        }
-        default: *d = 1.0f; return g;
+        *d = c + g * e * 0.39894228f;
+        return g * c;
+    } else if constexpr (ACT == ACT_RELU) {
+        *d = g > 0.0f ? 1.0f : 0.0f;
+        return g < 0.0f ? 0.0f : g;   // NaN stays
+    } else if constexpr (ACT == ACT_SIGMOID) {
+        const float s = sigmoid<E>(g);
+        *d = s * (1.0f - s);
+        return s;
+    } else {
+        *d = 1.0f;
+        return g;
     }
 }
 
-// Row m, columns n .. n + NV (as many as there are) of the product. g, u: the sums on entry;
+// f(constant) for the activation `act`
+template <class F>
+__device__ __forceinline__ void with_act(int act, F &&f) {
+    switch (act) {
+        case ACT_SILU: return f(std::integral_constant<int, ACT_SILU>());
+        case ACT_GELU: return f(std::integral_constant<int, ACT_GELU>());
+        case ACT_RELU: return f(std::integral_constant<int, ACT_RELU>());
+        case ACT_SIGMOID: return f(std::integral_constant<int, ACT_SIGMOID>());
+        default: return f(std::integral_constant<int, ACT_NONE>());
+    }
+}
+
+// What is the same for every row of some columns: biases (both projections'), or scales and bias.
+template <int NV>
+struct Columns {
+    float p[NV], q[NV];
+};
+
+template <int E, int EPI, int NV>
+__device__ __forceinline__ void load_columns(const DenseArgs &a, int64_t n, Columns<NV> &c) {
+    const int64_t count = a.N - n;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) c.p[v] = c.q[v] = 0.0f;
+    if (count <= 0) return;
+    if constexpr (EPI == DENSE_I8) {
+        load_wide<ELEM_F32, NV>(a.sw, n, count, c.p);
+        if (a.bias0) load_wide<ELEM_F32, NV>(a.bias0, n, count, c.q);
+    } else if constexpr (EPI == DENSE_GATED || EPI == DENSE_GATED_BWD) {
+        if (a.bias0) load_wide<E, NV>(a.bias0, n, count, c.p);
+        if (a.bias1) load_wide<E, NV>(a.bias1, n, count, c.q);
+    }
+}
+
+// Row m, columns n .. n + NV (as many as there are: at least one) of the product. g, u: the sums on entry;
 // DENSE_GATED_BWD leaves dG, dU there (0 beyond the last column).
-template <int E, int EPI, int NV, bool DUAL, class Sum>
-__device__ __forceinline__ void finish(const DenseArgs &a, int64_t split, int64_t m, int64_t n, Sum *g, Sum *u) {
+template <int E, int EPI, int ACT, int NV, bool DUAL, class Sum>
+__device__ __forceinline__ void finish(const DenseArgs &a, int64_t split, int64_t m, int64_t n, const Columns<NV> &c,
+                                       Sum *g, Sum *u) {
     const int64_t count = a.N - n;
     if constexpr (EPI == DENSE_PART) {
         const int64_t C = DUAL ? 2 * a.N : a.N;
         Sum *p = (Sum *)a.part + (split * a.M + m) * C + n;
-#pragma unroll
-        for (int h = 0; h < (DUAL ? 2 : 1); ++h) {
-            const Sum *s = h ? u : g;
-            typedef Sum Vec __attribute__((ext_vector_type(4), aligned(4)));
-#pragma unroll
-            for (int v = 0; v < NV; v += 4) {
-                if (v + 4 <= count) {
-                    *reinterpret_cast<Vec *>(p + h * a.N + v) = Vec{s[v], s[v + 1], s[v + 2], s[v + 3]};
-                } else {
-#pragma unroll
-                    for (int i = v; i < v + 4; ++i)
-                        if (i < count) p[h * a.N + i] = s[i];
-                }
-            }
-        }
+        store_wide<ELEM_F32, NV>(p, 0, count, (const float *)g);   // 32-bit words, also of integers
+        if constexpr (DUAL) store_wide<ELEM_F32, NV>(p, a.N, count, (const float *)u);
     } else if constexpr (EPI == DENSE_PLAIN) {
+        // rows from rows0 on are the second output's; between the two there may be rows of padding
         const bool second = a.out1 && m >= a.rows0;
-        store_wide<E, NV>(second ? a.out1 : a.out, (second ? m - a.rows0 : m) * a.ldo + n, count, (const float *)g);
+        const int64_t row = second ? m - a.rows0 : m;
+        if (!a.out1 || row < a.rows1)
+            store_wide<E, NV>(second ? a.out1 : a.out, row * a.ldo + n, count, (const float *)g);
     } else if constexpr (EPI == DENSE_I8) {
-        float y[NV], sw[NV], bias[NV];
+        float y[NV];
         const float sx = a.sx[m];
-        load_wide<ELEM_F32, NV>(a.sw, n, count, sw);
-        if (a.bias0) load_wide<ELEM_F32, NV>(a.bias0, n, count, bias);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            y[v] = (float)g[v] * sx * sw[v];
-            if (a.bias0) y[v] += bias[v];
-        }
+        for (int v = 0; v < NV; ++v) y[v] = (float)g[v] * sx * c.p[v] + c.q[v];
         if (a.out_elem == ELEM_BF16) store_wide<ELEM_BF16, NV>(a.out, m * a.ldo + n, count, y);
         else if (a.out_elem == ELEM_F16) store_wide<ELEM_F16, NV>(a.out, m * a.ldo + n, count, y);
         else store_wide<ELEM_F32, NV>(a.out, m * a.ldo + n, count, y);
+    } else if constexpr (EPI == DENSE_GATED) {
+        float y[NV], d;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) y[v] = activate<E, ACT>(g[v] + c.p[v], &d) * (u[v] + c.q[v]);
+        if (a.drop.on) {
+#pragma unroll
+            for (int v = 0; v < NV; v += 4) drop4(y + v, (uint32_t)((n + v) >> 2), (uint32_t)m, a.drop);
+        }
+        store_wide<E, NV>(a.out, m * a.ldo + n, count, y);
     } else {
-        if (a.bias0) {
-            float b[NV];
-            load_wide<E, NV>(a.bias0, n, count, b);
+        float y[NV];
+        load_wide<E, NV>(a.grad, m * a.ldg + n, count, y);   // 0 beyond the last column
+        if (a.drop.on) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) g[v] += b[v];
+            for (int v = 0; v < NV; v += 4) drop4(y + v, (uint32_t)((n + v) >> 2), (uint32_t)m, a.drop);
         }
-        if (a.bias1) {
-            float b[NV];
-            load_wide<E, NV>(a.bias1, n, count, b);
 #pragma unroll
-            for (int v = 0; v < NV; ++v) u[v] += b[v];
+        for (int v = 0; v < NV; ++v) {
+            float d;
+            const float h = activate<E, ACT>(g[v] + c.p[v], &d);
+            const bool in = v < count;
+            g[v] = in ? y[v] * (u[v] + c.q[v]) * d : 0.0f;
+            u[v] = in ? y[v] * h : 0.0f;
         }
-        if constexpr (EPI == DENSE_GATED) {
-            float y[NV], d;
+        store_wide<E, NV>(a.out, m * a.ldo + n, count, g);
+        store_wide<E, NV>(a.out1, m * a.ldo + n, count, u);
+    }
+}
+
+// The epilogue of a lane's accumulators: rows m + 16 i, columns n + 16 j + v in groups of NV, where groups
+// of 4 * PF are one run. csrow: the row of `colsum` that takes the sums over these rows.
+template <int E, int EPI, int FM, int FN, int PF, bool DUAL, int NV, class Acc>
+__device__ __forceinline__ void epilogue(const DenseArgs &a, int64_t split, int64_t m, int64_t n, Acc (&acc)[FM][FN],
+                                         int64_t csrow, int r16) {
+    typedef typename std::conditional<E == ELEM_I8, int, float>::type Sum;
+    constexpr int FG = NV / 4;   // fragments of one group
 #pragma unroll
-            for (int v = 0; v < NV; ++v) y[v] = activate<E>(a.act, g[v], &d) * u[v];
-            if (a.drop.on) {
+    for (int j = 0; j < PF; j += FG) {
+        const int64_t nj = n + 16 * j;
+        Columns<NV> c;
+        load_columns<E, EPI, NV>(a, nj, c);
+        auto rows = [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+            float csg[NV], csu[NV];
 #pragma unroll
-                for (int v = 0; v < NV; v += 4) drop4(y + v, (uint32_t)((n + v) >> 2), (uint32_t)m, a.drop);
+            for (int v = 0; v < NV; ++v) csg[v] = csu[v] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                if (m + 16 * i < a.M && nj < a.N) {
+                    Sum g[NV], u[NV];
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) {
+                        g[v] = acc[i][j + v / 4][v % 4];
+                        if constexpr (DUAL) u[v] = acc[i][PF + j + v / 4][v % 4];
+                    }
+                    finish<E, EPI, ACT, NV, DUAL>(a, split, m + 16 * i, nj, c, g, u);
+                    if constexpr (EPI == DENSE_GATED_BWD) {
+#pragma unroll
+                        for (int v = 0; v < NV; ++v) {
+                            csg[v] += g[v];
+                            csu[v] += u[v];
+                        }
+                    }
+                }
             }
-            store_wide<E, NV>(a.out, m * a.ldo + n, count, y);
-        } else {
-            float y[NV];
-            load_wide<E, NV>(a.grad, m * a.ldg + n, count, y);
-            if (a.drop.on) {
+            if constexpr (EPI == DENSE_GATED_BWD) {
+                if (a.colsum) {
+                    float *dst = a.colsum + csrow * 2 * a.N;
 #pragma unroll
-                for (int v = 0; v < NV; v += 4) drop4(y + v, (uint32_t)((n + v) >> 2), (uint32_t)m, a.drop);
-            }
+                    for (int v = 0; v < NV; ++v) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                float d;
-                const float h = activate<E>(a.act, g[v], &d);
-                g[v] = v < count ? y[v] * u[v] * d : 0.0f;
-                u[v] = v < count ? y[v] * h : 0.0f;
+                        for (int o = 1; o < 16; o <<= 1) {
+                            csg[v] += __shfl_xor(csg[v], o);
+                            csu[v] += __shfl_xor(csu[v], o);
+                        }
+                        if (r16 == 0 && nj + v < a.N) {
+                            dst[nj + v] = csg[v];
+                            dst[a.N + nj + v] = csu[v];
+                        }
+                    }
+                }
             }
-            store_wide<E, NV>(a.out, m * a.ldo + n, count, g);
-            store_wide<E, NV>(a.out1, m * a.ldo + n, count, u);
-        }
+        };
+        if constexpr (EPI == DENSE_GATED || EPI == DENSE_GATED_BWD) with_act(a.act, rows);
+        else rows(std::integral_constant<int, ACT_NONE>());
     }
 }
 

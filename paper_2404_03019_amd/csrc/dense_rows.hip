@@ -1,5 +1,5 @@
-// The dense operators' passes over rows: dropout, quantisation, the join of a product's parts,
-// transposition and the bias gradients' sums.
+// The dense operators' passes over rows: dropout, quantisation, the join of a product's parts
+// and the bias gradients' sums.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -104,25 +104,12 @@ __global__ void __launch_bounds__(kRowsBlock) join_kernel(const DenseArgs a) {
                     if constexpr (DUAL) u[j] += p[a.N + j];
                 }
         }
-        finish<E, EPI, 4, DUAL>(a, 0, m, n, g, u);
-    }
-}
-
-// tiles of 64 x 64 through LDS
-template <class V>
-__global__ void __launch_bounds__(kRowsBlock) transpose2d_kernel(const V *in, int64_t ldi, int64_t rows, int64_t cols,
-                                                                 V *out, int64_t ldo, int64_t tiles_c) {
-    __shared__ V tile[64][65];
-    const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    for (int i = w; i < 64; i += 4) {
-        const int64_t r = tr * 64 + i, c = tc * 64 + lane;
-        if (r < rows && c < cols) tile[i][lane] = in[r * ldi + c];
-    }
-    __syncthreads();
-    for (int i = w; i < 64; i += 4) {
-        const int64_t c = tc * 64 + i, r = tr * 64 + lane;
-        if (r < rows && c < cols) out[c * ldo + r] = tile[lane][i];
+        Columns<4> c;
+        load_columns<E, EPI, 4>(a, n, c);
+        if constexpr (EPI == DENSE_GATED)
+            with_act(a.act, [&](auto act) { finish<E, EPI, decltype(act)::value, 4, DUAL>(a, 0, m, n, c, g, u); });
+        else
+            finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, c, g, u);
     }
 }
 
@@ -211,21 +198,6 @@ hipError_t launch_dense_join(int elem, int epi, const DenseArgs &a, hipStream_t 
     if (elem == ELEM_BF16) return join_float<ELEM_BF16>(epi, a, st);
     if (elem == ELEM_F16) return join_float<ELEM_F16>(epi, a, st);
     return hipErrorInvalidValue;
-}
-
-hipError_t launch_transpose2d(int elem, const void *in, int64_t ldi, int64_t rows, int64_t cols, void *out, int64_t ldo,
-                              hipStream_t st) {
-    const int64_t tc = (cols + 63) / 64, tr = (rows + 63) / 64;
-    if (tc * tr == 0) return hipSuccess;
-    if (tc > INT32_MAX / tr) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)(tc * tr));
-    if (elem == ELEM_F32)
-        hipLaunchKernelGGL(transpose2d_kernel<uint32_t>, grid, dim3(kRowsBlock), 0, st, (const uint32_t *)in, ldi, rows,
-                           cols, (uint32_t *)out, ldo, tc);
-    else
-        hipLaunchKernelGGL(transpose2d_kernel<uint16_t>, grid, dim3(kRowsBlock), 0, st, (const uint16_t *)in, ldi, rows,
-                           cols, (uint16_t *)out, ldo, tc);
-    return hipGetLastError();
 }
 
 hipError_t launch_colsum(int elem, const float *colsum, int64_t rows, int64_t N, float *mid, void *out0, void *out1,

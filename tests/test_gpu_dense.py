@@ -162,9 +162,9 @@ def test_gated_larger(dtype, M, K, N):
         ref.check(t, *w, f"gradient {i}")
 
 
-@pytest.mark.parametrize("dtype", (BF16, F32))
-def test_gated_large_tiles(dtype):
-    M, K, N = 16_500, 72, 520
+@pytest.mark.parametrize("dtype, M, K, N", [(BF16, 16_500, 72, 520), (F32, 16_500, 72, 520), (BF16, 4_200, 456, 2_056),
+                                            (F16, 4_200, 640, 2_072), (F32, 4_200, 228, 2_060)])
+def test_gated_large_tiles(dtype, M, K, N):
     g = gen(6)
     x, wg, wu = rand(g, M, K, dtype=dtype), rand(g, N, K, dtype=dtype, scale=0.1), rand(g, N, K, dtype=dtype, scale=0.1)
     grad = rand(g, M, N, dtype=dtype)
@@ -330,9 +330,10 @@ def test_int8_extreme_sums():
     assert (got.double() == float(np.float32(128.0 * 128.0 * K))).all()
 
 
-def test_int8_large_tiles():
+@pytest.mark.parametrize("K", (200, 1040, 1280))
+def test_int8_large_tiles(K):
     g = gen(12)
-    M, K, N = 5000, 200, 4100
+    M, N = 5000, 4100
     xq = torch.randint(-127, 128, (M, K), generator=g, device=DEV).to(torch.int8)
     wq = torch.randint(-127, 128, (N, K), generator=g, device=DEV).to(torch.int8)
     sx, sw = torch.rand(M, generator=g, device=DEV), torch.rand(N, generator=g, device=DEV)

@@ -11,6 +11,7 @@
 
 namespace geot {
 
+constexpr int64_t kDenseCUs = 256;
 constexpr int ELEM_I8 = 3;  // beside ElemType: the 8-bit product's operands
 
 enum ActFn : int { ACT_SILU = 0, ACT_GELU = 1, ACT_RELU = 2, ACT_SIGMOID = 3, ACT_NONE = 4 };
@@ -31,7 +32,8 @@ enum DenseMode : int {
     DENSE_TN = 2,  // both have a row per k
 };
 
-enum DenseTile : int { DENSE_TILE_128 = 0, DENSE_TILE_256 = 1 };
+// DENSE_TILE_SMALL: blocks of 16 fm rows and 16 fn weight rows, whose waves share K
+enum DenseTile : int { DENSE_TILE_128 = 0, DENSE_TILE_256 = 1, DENSE_TILE_SMALL = 2 };
 
 // C[m, n] = sum_k A[m, k] B[n, k]. With DENSE_NT and b1 there are two column operands: g comes from b0 and u
 // from b1, N columns each. With DENSE_NN and b1 K comes twice: A's second K columns start seg_a bytes
@@ -62,6 +64,7 @@ struct DenseArgs {
 // Tile and split of a product, chosen by plan_dense from its sizes.
 struct DensePlan {
     int tile;         // DenseTile
+    int fm, fn;       // DENSE_TILE_SMALL
     bool direct;      // whole steps are loaded straight into LDS
     int64_t splits;   // parts of K; more than one takes `part` and a join
     int64_t steps_per;
@@ -71,11 +74,12 @@ struct DensePlan {
 };
 
 // dual: two column operands (DENSE_NT); segments: of K (DENSE_NN)
-DensePlan plan_dense(int elem, int epi, int64_t M, int64_t N, int64_t K, bool dual, int segments, bool direct);
+DensePlan plan_dense(int elem, int epi, int mode, int64_t M, int64_t N, int64_t K, bool dual, int segments, bool direct);
 // Runs the product (and the join of its parts) with `epi`; a.part holds plan.part_bytes.
 hipError_t launch_dense(int elem, int epi, int mode, DenseArgs a, const DensePlan &plan, hipStream_t st);
 #define GEOT_DENSE_LAUNCHER(NAME) \
-    hipError_t NAME(int epi, int mode, int tile, bool direct, const DenseArgs &a, int64_t blocks, hipStream_t st)
+    hipError_t NAME(int epi, int mode, int tile, int fm, int fn, bool direct, const DenseArgs &a, int64_t blocks, \
+                    hipStream_t st)
 GEOT_DENSE_LAUNCHER(launch_dense_f32);
 GEOT_DENSE_LAUNCHER(launch_dense_bf16);
 GEOT_DENSE_LAUNCHER(launch_dense_f16);

@@ -14,7 +14,6 @@
 namespace geot {
 namespace {
 
-constexpr int kChipCUs = 256;
 constexpr int64_t kMaxInt8K = 131071;  // (-128)(-128) K stays below 2^31
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -112,18 +111,36 @@ static bool direct_ok(const void *p, int64_t ld, int64_t es, int64_t cols = 0) {
     return ((uintptr_t)p & 15) == 0 && ld * es % 16 == 0 && ld * es < ((int64_t)1 << 23) && cols * es % 16 == 0;
 }
 
-DensePlan plan_dense(int elem, int epi, int64_t M, int64_t N, int64_t K, bool dual, int segments, bool direct) {
-    DensePlan p{DENSE_TILE_128, direct, 1, 0, 0, 0, 0, 0};
+DensePlan plan_dense(int elem, int epi, int mode, int64_t M, int64_t N, int64_t K, bool dual, int segments, bool direct) {
+    DensePlan p{DENSE_TILE_128, 0, 0, direct, 1, 0, 0, 0, 0, 0};
     const int64_t steps = K * elem_bytes(elem) / 128 * segments, C = dual ? 2 * N : N;   // whole steps
-    const int64_t t_big = up(M, 256) * up(C, 256);
-    if (direct && t_big >= kChipCUs) p.tile = DENSE_TILE_256;
+    // 256 x 256 tiles (one block a CU) take a step in 1.6 us and 7 us besides, 128 x 128 ones (two a CU) 1.0
+    // and 3; whichever gets through its rounds sooner. Measured, gated block, bf16, 256 / 128: 16,384 rows,
+    // 2,048 -> 8,192 934 / 1,130 us; 1,024 -> 2,048 135 / 151; 512 -> 1,024 45 / 47; 170,003 rows, 128 -> 256
+    // 66 / 55. fp32, whose multiplications take eight times as long, gains nothing from the larger tile
+    // (16,384 rows, 1,024 -> 2,048 1,059 / 1,056 us).
+    const int64_t t_big = up(M, 256) * up(C, 256), t_small = up(M, 128) * up(C, 128);
+    if (mode == DENSE_NT && (M <= 64 || t_small < kDenseCUs / 2)) {
+        // Few rows, or tiles for less than half the chip: blocks of up to 64 rows whose waves share K. As many
+        // weight rows a block as still give every CU a block.
+        p.tile = DENSE_TILE_SMALL;
+        p.fm = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+        p.tiles_m = up(M, 16 * p.fm);
+        p.fn = p.tiles_m * up(C, 64) >= kDenseCUs ? 4 : dual ? 2 : 1;
+        p.tiles_n = up(N, dual ? 8 * p.fn : 16 * p.fn);
+        p.colsum_rows = p.tiles_m * p.fm;
+        return p;
+    }
+    if (direct && elem != ELEM_F32 && t_big >= kDenseCUs &&
+        up(t_big, kDenseCUs) * (70 + 16 * steps) < up(t_small, 2 * kDenseCUs) * (30 + 10 * steps))
+        p.tile = DENSE_TILE_256;
     const int64_t tile = p.tile == DENSE_TILE_256 ? 256 : 128;
     p.tiles_m = up(M, tile);
     p.tiles_n = up(N, dual ? tile / 2 : tile);
     const int64_t tiles = std::max<int64_t>(1, p.tiles_m * p.tiles_n);
     p.steps_per = std::max<int64_t>(steps, 1);
-    if (epi != DENSE_GATED_BWD && tiles < kChipCUs && steps > 1) {
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2 * kChipCUs / tiles, steps / 4));
+    if (epi != DENSE_GATED_BWD && tiles < kDenseCUs && steps > 1) {
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2 * kDenseCUs / tiles, steps / 4));
         p.steps_per = up(up(steps, want), 2) * 2;   // even: the kernel takes steps in pairs
         p.splits = up(steps, p.steps_per);
     }
@@ -142,10 +159,10 @@ hipError_t launch_dense(int elem, int epi, int mode, DenseArgs a, const DensePla
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const int e = plan.splits > 1 ? DENSE_PART : epi;
     hipError_t r = hipErrorInvalidValue;
-    if (elem == ELEM_F32) r = launch_dense_f32(e, mode, plan.tile, plan.direct, a, blocks, st);
-    else if (elem == ELEM_BF16) r = launch_dense_bf16(e, mode, plan.tile, plan.direct, a, blocks, st);
-    else if (elem == ELEM_F16) r = launch_dense_f16(e, mode, plan.tile, plan.direct, a, blocks, st);
-    else if (elem == ELEM_I8) r = launch_dense_i8(e, mode, plan.tile, plan.direct, a, blocks, st);
+    if (elem == ELEM_F32) r = launch_dense_f32(e, mode, plan.tile, plan.fm, plan.fn, plan.direct, a, blocks, st);
+    else if (elem == ELEM_BF16) r = launch_dense_bf16(e, mode, plan.tile, plan.fm, plan.fn, plan.direct, a, blocks, st);
+    else if (elem == ELEM_F16) r = launch_dense_f16(e, mode, plan.tile, plan.fm, plan.fn, plan.direct, a, blocks, st);
+    else if (elem == ELEM_I8) r = launch_dense_i8(e, mode, plan.tile, plan.fm, plan.fn, plan.direct, a, blocks, st);
     if (r != hipSuccess || plan.splits == 1) return r;
     return launch_dense_join(elem, epi, a, st);
 }
@@ -194,7 +211,7 @@ geot_status_t gated_forward(const Gated &q, geot_activation_t act, const Drop &d
     a.drop = drop;
     a.out = const_cast<void *>(out.p);
     a.ldo = out.ld;
-    const DensePlan plan = plan_dense(q.elem, DENSE_GATED, q.M, q.N, q.K, true, 1, gated_direct(q));
+    const DensePlan plan = plan_dense(q.elem, DENSE_GATED, DENSE_NT, q.M, q.N, q.K, true, 1, gated_direct(q));
     CallMemory mem(st);
     char *part = nullptr;
     DENSE_TRY(mem.get(plan.part_bytes, &part));
@@ -291,10 +308,10 @@ geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stri
         // dG and dU side by side in the storage type, [M x Np] each: the rounding that the gradients of two
         // separate projections would have. Each starts on 16 bytes in every row.
         const int64_t lane = 16 / es, Np = up(N, lane) * lane, ld2 = 2 * Np;
-        const DensePlan p0 = plan_dense(elem, DENSE_GATED_BWD, M, N, K, true, 1, gated_direct(q));
-        const DensePlan px = plan_dense(elem, DENSE_PLAIN, M, K, N, false, 2,
+        const DensePlan p0 = plan_dense(elem, DENSE_GATED_BWD, DENSE_NT, M, N, K, true, 1, gated_direct(q));
+        const DensePlan px = plan_dense(elem, DENSE_PLAIN, DENSE_NN, M, K, N, false, 2,
                                         direct_ok(w_gate, w_stride, es, K) && direct_ok(w_up, w_stride, es, K) && ld2 * es < ((int64_t)1 << 23));
-        const DensePlan pw = plan_dense(elem, DENSE_PLAIN, ld2, K, M, false, 1,
+        const DensePlan pw = plan_dense(elem, DENSE_PLAIN, DENSE_TN, ld2, K, M, false, 1,
                                         direct_ok(x, x_stride, es, K) && ld2 * es < ((int64_t)1 << 23));
         size_t at = 0;
         auto take = [&](size_t b) {
@@ -421,7 +438,7 @@ geot_status_t geot_linear_int8(const int8_t *xq, const float *x_scale, int64_t r
         a.out = out;
         a.out_elem = (int)out_type;
         a.ldo = out_stride;
-        const DensePlan plan = plan_dense(ELEM_I8, DENSE_I8, M, N, K, false, 1, direct_ok(xq, x_stride, 1) && direct_ok(wq, w_stride, 1));
+        const DensePlan plan = plan_dense(ELEM_I8, DENSE_I8, DENSE_NT, M, N, K, false, 1, direct_ok(xq, x_stride, 1) && direct_ok(wq, w_stride, 1));
         CallMemory mem(st);
         char *part = nullptr;
         DENSE_TRY(mem.get(plan.part_bytes, &part));

@@ -1,8 +1,16 @@
 // Products of the dense operators, f16 operands.
 #include "dense_kernel.h"
+#include "dense_small.h"
 
 namespace geot {
 
-GEOT_DENSE_LAUNCHER(launch_dense_f16) { return launch_float<ELEM_F16>(epi, mode, tile, direct, a, blocks, st); }
+GEOT_DENSE_LAUNCHER(launch_dense_f16) {
+    if (tile == DENSE_TILE_SMALL) {
+        if (epi == DENSE_GATED) return launch_small<ELEM_F16, DENSE_GATED, true>(a, fm, fn, blocks, st);
+        if (epi == DENSE_GATED_BWD) return launch_small<ELEM_F16, DENSE_GATED_BWD, true>(a, fm, fn, blocks, st);
+        return hipErrorInvalidValue;
+    }
+    return launch_float<ELEM_F16>(epi, mode, tile, direct, a, blocks, st);
+}
 
 }  // namespace geot

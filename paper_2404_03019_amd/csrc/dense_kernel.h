@@ -90,18 +90,28 @@ __device__ __forceinline__ void mma_pinned(chunk_t w, chunk_t x, typename AccOf<
         asm("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
     } else if constexpr (E == ELEM_F16) {
         asm("s_nop 1\n\tv_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
-    } else if constexpr (E == ELEM_I8) {
-        asm("s_nop 1\n\tv_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
     } else {
-        const f32x4 a = __builtin_bit_cast(f32x4, w), b = __builtin_bit_cast(f32x4, x);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) asm("s_nop 1\n\tv_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(acc) : "v"(a[j]), "v"(b[j]));
+        static_assert(E == ELEM_I8, "the large tile is for 16- and 8-bit operands");
+        asm("s_nop 1\n\tv_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
     }
 }
-// between the last of these and the first other use of the sums: the wait states of the longest MFMA
+// the first of a sum: no zeros to write before
+template <int E>
+__device__ __forceinline__ void mma_first(chunk_t w, chunk_t x, typename AccOf<E>::type &acc) {
+    if constexpr (E == ELEM_BF16) {
+        asm("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(acc) : "v"(w), "v"(x));
+    } else if constexpr (E == ELEM_F16) {
+        asm("s_nop 1\n\tv_mfma_f32_16x16x32_f16 %0, %1, %2, 0" : "=a"(acc) : "v"(w), "v"(x));
+    } else {
+        asm("s_nop 1\n\tv_mfma_i32_16x16x64_i8 %0, %1, %2, 0" : "=a"(acc) : "v"(w), "v"(x));
+    }
+}
+// Between the last of these and the first other use of the sums: the wait states of the longest MFMA, once,
+// and then every sum passes here after it.
+__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15"); }
 template <class Acc>
-__device__ __forceinline__ void settle(Acc &acc) {
-    asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc));
+__device__ __forceinline__ void settled(Acc &acc) {
+    asm volatile("" : "+a"(acc));
 }
 
 // 16 bytes at p, of which `left` may be read (any number); bytes beyond are 0. What is read ends a run of at
@@ -216,6 +226,7 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
     const uint32_t per = 8 * tiles_n, grp = t / per, gm = tiles_m - grp * 8 < 8 ? tiles_m - grp * 8 : 8;
     const uint32_t in = t - grp * per, tn = in / gm, tm = grp * 8 + (in - tn * gm);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * HB;
+    const int64_t mleft = a.M - m0, nleft = a.N - n0;   // rows (columns) of the tile that exist: at least 1
 
     // Steps of K. This split's whole ones are [s0, s1), of each segment in turn (DENSE_NN: two); the first
     // split also takes the step that ends each segment short. The host gives every split but the last an even
@@ -231,10 +242,11 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % WM, wn = wave / WM, r16 = lane & 15, c4 = lane >> 4;
 
+    const int64_t lda = a.lda * ES, ldb = a.ldb * ES;
+    const int64_t inca = KA ? TA::KS * lda : kStepBytes, incb = KB ? TB::KS * ldb : kStepBytes;
+
     // Where a thread's chunks come from, relative to the tile's (and step's) first element. Rows and
     // columns beyond the end read others in their place; what they give is never stored.
-    const int64_t lda = a.lda * ES, ldb = a.ldb * ES;
-    const int64_t mleft = a.M - m0, nleft = a.N - n0;   // rows (columns) of the tile that exist: at least 1
     auto place = [&](auto tile, int i, int64_t left, int64_t *row, int *byte, int fold) {
         typedef decltype(tile) TT;
         const int r = TT::row_of(i), c = TT::chunk_of(i) * 16;
@@ -247,28 +259,26 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
             *byte = c;
         }
     };
-    // direct loads: 32-bit offsets (the host has checked that they fit)
-    uint32_t oa[CA], ob[CB];
+    const char *const basea = (const char *)a.a + (KA ? m0 * ES : m0 * lda);
+    const char *const baseb = (const char *)a.b0 + (KB ? n0 * ES : n0 * ldb);
+    const char *const baseb1 = a.b1 ? (const char *)a.b1 + (KB ? n0 * ES : n0 * ldb) : nullptr;
+    uint32_t oa[CA], ob[CB];   // direct loads: 32-bit offsets (the host has checked that they fit)
     if constexpr (DIRECT) {
 #pragma unroll
         for (int c = 0; c < CA; ++c) {
             int64_t row;
             int byte;
             place(TA{}, tid + c * T, mleft, &row, &byte, BM);
-            oa[c] = (uint32_t)(row * lda) + byte;
+            oa[c] = (uint32_t)row * (uint32_t)lda + byte;
         }
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
             int64_t row;
             int byte;
             place(TB{}, tid + c * T, nleft, &row, &byte, HB);
-            ob[c] = (uint32_t)(row * ldb) + byte;
+            ob[c] = (uint32_t)row * (uint32_t)ldb + byte;
         }
     }
-    const char *const basea = (const char *)a.a + (KA ? m0 * ES : m0 * lda);
-    const char *const baseb = (const char *)a.b0 + (KB ? n0 * ES : n0 * ldb);
-    const char *const baseb1 = a.b1 ? (const char *)a.b1 + (KB ? n0 * ES : n0 * ldb) : nullptr;
-    const int64_t inca = KA ? TA::KS * lda : kStepBytes, incb = KB ? TB::KS * ldb : kStepBytes;
 
     const bool narrow_a = (KA ? a.M : a.K) * ES < 16, narrow_b = (KB ? a.N : a.K) * ES < 16;
     struct Source {
@@ -334,10 +344,6 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
         brow[j] = (j / PF) * HB + wn * (16 * PF) + (KB ? 16 * f : 4 * PF * (r16 >> 2) + 4 * f + (r16 & 3));
     }
     Acc acc[FM][FN];
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
 
     struct Frags {
         chunk_t x[FM], w[FN];
@@ -387,45 +393,61 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
             land(lds);
         }
     }
+    turn();
     if constexpr (PINNED) {
         // One wave a SIMD: the next half's operands are read while this one's are multiplied, in this order:
         // those that the next half needs first come first.
         Frags f0, f1;
+        auto read_part = [&](Frags &next, const char *lds, int kk, int i) {
+#pragma unroll
+            for (int r = i * (FN + FM) / FM; r < (i + 1) * (FN + FM) / FM; ++r) {
+                if (r < FN) read_w(next, lds, kk, r);
+                else read_x(next, lds, kk, r - FN);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
         auto phase = [&](const Frags &now, Frags &next, const char *lds, int kk) {
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-#pragma unroll
-                for (int r = i * (FN + FM) / FM; r < (i + 1) * (FN + FM) / FM; ++r) {
-                    if (r < FN) read_w(next, lds, kk, r);
-                    else read_x(next, lds, kk, r - FN);
-                }
-                __builtin_amdgcn_sched_barrier(0);
+                read_part(next, lds, kk, i);
                 multiply(now, i);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-        turn();
 #pragma unroll
-        for (int j = 0; j < FN; ++j) read_w(f0, lds0, 0, j);
+        for (int i = 0; i < FM; ++i) read_part(f0, lds0, 0, i);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) read_x(f0, lds0, 0, i);
-        for (int64_t j = 2;; j += 2) {
-            phase(f0, f1, lds0, 1);
+        for (int i = 0; i < FM; ++i) {
+            read_part(f1, lds0, 1, i);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) mma_first<E>(f0.w[j], f0.x[i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        for (int64_t j = 2; j < slots; j += 2) {
             turn();
-            const bool more = j < slots;
-            if (more) issue(lds0, j);
+            issue(lds0, j);
             phase(f1, f0, lds1, 0);
             phase(f0, f1, lds1, 1);
             turn();
-            if (more) issue(lds1, j + 1);
-            phase(f1, f0, lds0, 0);   // after the last pair what is read here is not used
-            if (!more) break;
+            issue(lds1, j + 1);
+            phase(f1, f0, lds0, 0);
+            phase(f0, f1, lds0, 1);
         }
+        turn();
+        phase(f1, f0, lds1, 0);
+        phase(f0, f1, lds1, 1);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) multiply(f1, i);
+        settle();
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) settle(acc[i][j]);
+            for (int j = 0; j < FN; ++j) settled(acc[i][j]);
     } else {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
         Frags f;
         auto product = [&](const char *lds) {
 #pragma unroll
@@ -438,7 +460,6 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
                 for (int i = 0; i < FM; ++i) multiply(f, i);
             }
         };
-        turn();
         for (int64_t j = 2;; j += 2) {
             product(lds0);
             turn();
@@ -452,7 +473,6 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
             land(lds1);
         }
     }
-
     epilogue<E, EPI, FM, FN, PF, DUAL, KB ? 4 : 4 * PF>(a, split, m0 + wm * (BM / WM) + r16,
                                                         n0 + wn * (16 * PF) + (KB ? 4 : 4 * PF) * c4, acc,
                                                         (int64_t)tm * WM + wm, r16);
@@ -461,9 +481,13 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
 template <int E, int EPI, bool DUAL, int MODE>
 hipError_t launch_tile(int tile, bool direct, const DenseArgs &a, int64_t blocks, hipStream_t st) {
     const dim3 grid((unsigned)blocks);
-    if (tile == DENSE_TILE_256)
-        hipLaunchKernelGGL((dense_kernel<E, 256, 256, 2, 2, EPI, DUAL, MODE, true>), grid, dim3(256), 0, st, a);
-    else if (direct)
+    if constexpr (E != ELEM_F32) {
+        if (tile == DENSE_TILE_256) {
+            hipLaunchKernelGGL((dense_kernel<E, 256, 256, 2, 2, EPI, DUAL, MODE, true>), grid, dim3(256), 0, st, a);
+            return hipGetLastError();
+        }
+    }
+    if (direct)
         hipLaunchKernelGGL((dense_kernel<E, 128, 128, 2, 2, EPI, DUAL, MODE, true>), grid, dim3(256), 0, st, a);
     else
         hipLaunchKernelGGL((dense_kernel<E, 128, 128, 2, 2, EPI, DUAL, MODE, false>), grid, dim3(256), 0, st, a);

@@ -1,0 +1,161 @@
+// Products with few rows (a token, a handful of nodes), or too small to fill the chip with tiles.
+//
+// What bounds them is the read of the weights, once, and latency. A block of 8 waves takes 16 FM rows and
+// 16 FN weight rows; its waves share K (64 bytes of a row each in turn, so that neighbouring waves read
+// neighbouring bytes) and load the operands of the matrix instructions straight from memory, several steps
+// ahead, with no LDS and no barrier on the way. At the end the waves' sums are added through LDS in
+// a fixed order, and each thread finishes four columns of a row: one launch, nothing in memory between.
+#pragma once
+
+#include "dense_kernel.h"
+
+namespace geot {
+namespace {
+
+constexpr int kSmallWaves = 8;
+
+template <int E, int FM, int FN, int EPI, bool DUAL>
+__global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs a) {
+    constexpr int ES = E == ELEM_F32 ? 4 : E == ELEM_I8 ? 1 : 2;
+    constexpr int PF = DUAL ? FN / 2 : FN, HB = 16 * PF;   // columns of one operand
+    constexpr int U = FM + FN <= 4 ? 8 : 4;                // steps loaded ahead
+    constexpr int kUnits = FM * PF * 64;                   // four columns of a row each
+    typedef typename AccOf<E>::type Acc;
+    typedef typename AccOf<E>::scalar Sum;
+    __shared__ Acc part[kSmallWaves][FM * FN][64];
+
+    // neighbouring tiles on one chiplet: the row tiles of one column tile share its weights
+    const uint32_t nb = gridDim.x, b = blockIdx.x, x8 = b & 7, q8 = nb >> 3, r8 = nb & 7;
+    const uint32_t id = x8 * q8 + (x8 < r8 ? x8 : r8) + (b >> 3);
+    const uint32_t tn = id / (uint32_t)a.tiles_m, tm = id - tn * (uint32_t)a.tiles_m;
+    const int64_t m0 = (int64_t)tm * (16 * FM), n0 = (int64_t)tn * HB;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r16 = lane & 15, c4 = lane >> 4;
+
+    // rows and columns beyond the end read the last one; what they give is never stored
+    const char *px[FM], *pw[FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int64_t m = m0 + 16 * i + r16;
+        px[i] = (const char *)a.a + (m < a.M ? m : a.M - 1) * a.lda * ES + c4 * 16;
+    }
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int64_t n = n0 + 16 * (j % PF) + r16;
+        pw[j] = (const char *)(j < PF ? a.b0 : a.b1) + (n < a.N ? n : a.N - 1) * a.ldb * ES + c4 * 16;
+    }
+    Acc acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+
+    const int64_t kbytes = a.K * ES, whole = kbytes / 64;
+    const bool narrow = kbytes < 16;
+    auto steps = [&](auto count, int64_t s) {
+        constexpr int C = decltype(count)::value;
+        chunk_t x[C][FM], w[C][FN];
+#pragma unroll
+        for (int u = 0; u < C; ++u) {
+            const int64_t at = (s + kSmallWaves * u) * 64;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) w[u][j] = *reinterpret_cast<const chunk_any *>(pw[j] + at);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) x[u][i] = *reinterpret_cast<const chunk_any *>(px[i] + at);
+        }
+#pragma unroll
+        for (int u = 0; u < C; ++u)
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = mma<E>(w[u][j], x[u][i], acc[i][j]);
+    };
+    int64_t s = wave;
+    for (; s + kSmallWaves * (U - 1) < whole; s += kSmallWaves * U) steps(std::integral_constant<int, U>(), s);
+    if (s + kSmallWaves < whole) {
+        for (; s + kSmallWaves < whole; s += 2 * kSmallWaves) steps(std::integral_constant<int, 2>(), s);
+    }
+    if (s < whole) {
+        steps(std::integral_constant<int, 1>(), s);
+        s += kSmallWaves;
+    }
+    if (s == whole && whole * 64 < kbytes) {   // the step that K cuts short, in the wave whose turn it is
+        const int64_t left = kbytes - whole * 64 - c4 * 16;
+        chunk_t x[FM], w[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) w[j] = load_chunk<ES>(pw[j] + whole * 64, left, narrow);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) x[i] = load_chunk<ES>(px[i] + whole * 64, left, narrow);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = mma<E>(w[j], x[i], acc[i][j]);
+    }
+
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) part[wave][i * FN + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int unit = tid; unit < kUnits; unit += kSmallWaves * 64) {
+        const int i = unit / (PF * 64), j = unit / 64 % PF;
+        Acc vg = part[0][i * FN + j][lane], vu = Acc{0, 0, 0, 0};
+        if constexpr (DUAL) vu = part[0][i * FN + PF + j][lane];
+#pragma unroll
+        for (int w = 1; w < kSmallWaves; ++w) {
+            vg += part[w][i * FN + j][lane];
+            if constexpr (DUAL) vu += part[w][i * FN + PF + j][lane];
+        }
+        const int64_t m = m0 + 16 * i + r16, n = n0 + 16 * j + 4 * c4;
+        const bool in = m < a.M && n < a.N;
+        Sum g[4], u[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            g[v] = vg[v];
+            u[v] = vu[v];
+        }
+        if (in) {
+            Columns<4> c;
+            load_columns<E, EPI, 4>(a, n, c);
+            if constexpr (EPI == DENSE_GATED || EPI == DENSE_GATED_BWD)
+                with_act(a.act, [&](auto act) { finish<E, EPI, decltype(act)::value, 4, DUAL>(a, 0, m, n, c, g, u); });
+            else
+                finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, c, g, u);
+        }
+        if constexpr (EPI == DENSE_GATED_BWD) {
+            if (a.colsum) {   // a row of column sums for each 16 rows
+                float *dst = a.colsum + ((int64_t)tm * FM + i) * 2 * a.N;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    float sg = in ? g[v] : 0.0f, su = in ? u[v] : 0.0f;
+#pragma unroll
+                    for (int o = 1; o < 16; o <<= 1) {
+                        sg += __shfl_xor(sg, o);
+                        su += __shfl_xor(su, o);
+                    }
+                    if (r16 == 0 && n + v < a.N) {
+                        dst[n + v] = sg;
+                        dst[a.N + n + v] = su;
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <int E, int EPI, bool DUAL>
+hipError_t launch_small(const DenseArgs &a, int fm, int fn, int64_t blocks, hipStream_t st) {
+    const dim3 grid((unsigned)blocks), block(kSmallWaves * 64);
+    constexpr int FN = DUAL ? 2 : 1;
+    if (fn == FN && fm == 1) hipLaunchKernelGGL((small_kernel<E, 1, FN, EPI, DUAL>), grid, block, 0, st, a);
+    else if (fn == FN && fm == 2) hipLaunchKernelGGL((small_kernel<E, 2, FN, EPI, DUAL>), grid, block, 0, st, a);
+    else if (fn == FN && fm == 4) hipLaunchKernelGGL((small_kernel<E, 4, FN, EPI, DUAL>), grid, block, 0, st, a);
+    else if (fn == 4 && fm == 1) hipLaunchKernelGGL((small_kernel<E, 1, 4, EPI, DUAL>), grid, block, 0, st, a);
+    else if (fn == 4 && fm == 2) hipLaunchKernelGGL((small_kernel<E, 2, 4, EPI, DUAL>), grid, block, 0, st, a);
+    else if (fn == 4 && fm == 4) hipLaunchKernelGGL((small_kernel<E, 4, 4, EPI, DUAL>), grid, block, 0, st, a);
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace geot

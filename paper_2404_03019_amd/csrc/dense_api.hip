@@ -140,7 +140,7 @@ DensePlan plan_dense(int elem, int epi, int mode, int64_t M, int64_t N, int64_t 
     const int64_t tiles = std::max<int64_t>(1, p.tiles_m * p.tiles_n);
     p.steps_per = std::max<int64_t>(steps, 1);
     if (epi != DENSE_GATED_BWD && tiles < kDenseCUs && steps > 1) {
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2 * kDenseCUs / tiles, steps / 4));
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2 * kDenseCUs / tiles, steps / 2));
         p.steps_per = up(up(steps, want), 2) * 2;   // even: the kernel takes steps in pairs
         p.splits = up(steps, p.steps_per);
     }

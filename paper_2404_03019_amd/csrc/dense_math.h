@@ -33,7 +33,8 @@ struct Pack {
     typedef typename StoreOf<E>::type type __attribute__((ext_vector_type(V), aligned(sizeof(typename StoreOf<E>::type))));
 };
 
-// v[0..V) = p[0..V), the first `count` of them (the others 0)
+// v[0..V) = p[0..V), the first `count` of them (the others 0). A vector that a row cuts short moves in pieces
+// of halving size.
 template <int E, int V>
 __device__ __forceinline__ void load_wide(const void *base, int64_t at, int64_t count, float *v) {
     const auto *p = (const typename StoreOf<E>::type *)base + at;
@@ -45,10 +46,33 @@ __device__ __forceinline__ void load_wide(const void *base, int64_t at, int64_t 
 #pragma unroll
             for (int j = 0; j < S; ++j) v[i + j] = (float)x[j];
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = i < count ? (float)p[i] : 0.0f;
+        return;
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = 0.0f;
+    if (count <= 0) return;
+    const int n = (int)count;
+    // from the end: the pieces that have been loaded move up as the next one, twice as long, comes before them
+    auto piece = [&](auto size) {
+        constexpr int P = decltype(size)::value;
+        if constexpr (P < V) {
+            if (n & P) {
+#pragma unroll
+                for (int i = V - 1; i >= P; --i) v[i] = v[i - P];
+                constexpr int S2 = P < W ? P : W;
+#pragma unroll
+                for (int i = 0; i < P; i += S2) {
+                    const auto x = *reinterpret_cast<const typename Pack<E, S2>::type *>(p + (n & ~(2 * P - 1)) + i);
+#pragma unroll
+                    for (int j = 0; j < S2; ++j) v[i + j] = (float)x[j];
+                }
+            }
+        }
+    };
+    piece(std::integral_constant<int, 1>());
+    piece(std::integral_constant<int, 2>());
+    piece(std::integral_constant<int, 4>());
+    piece(std::integral_constant<int, 8>());
 }
 
 template <int E, int V>
@@ -63,11 +87,35 @@ __device__ __forceinline__ void store_wide(void *base, int64_t at, int64_t count
             for (int j = 0; j < S; ++j) x[j] = (typename StoreOf<E>::type)v[i + j];
             *reinterpret_cast<typename Pack<E, S>::type *>(p + i) = x;
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < count) p[i] = (typename StoreOf<E>::type)v[i];
+        return;
     }
+    if (count <= 0) return;
+    const int n = (int)count;
+    float y[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) y[i] = v[i];
+    // from the start: what follows a piece that has been stored moves down
+    auto piece = [&](auto size) {
+        constexpr int P = decltype(size)::value;
+        if constexpr (P < V) {
+            if (n & P) {
+                constexpr int S2 = P < W ? P : W;
+#pragma unroll
+                for (int i = 0; i < P; i += S2) {
+                    typename Pack<E, S2>::type x;
+#pragma unroll
+                    for (int j = 0; j < S2; ++j) x[j] = (typename StoreOf<E>::type)y[i + j];
+                    *reinterpret_cast<typename Pack<E, S2>::type *>(p + (n & ~(2 * P - 1)) + i) = x;
+                }
+#pragma unroll
+                for (int i = 0; i + P < V; ++i) y[i] = y[i + P];
+            }
+        }
+    };
+    piece(std::integral_constant<int, 8>());
+    piece(std::integral_constant<int, 4>());
+    piece(std::integral_constant<int, 2>());
+    piece(std::integral_constant<int, 1>());
 }
 
 // 16-bit results take the short exponential and reciprocal (a few units of the 24th bit), fp32 ones the

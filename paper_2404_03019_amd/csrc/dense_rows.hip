@@ -17,24 +17,44 @@ unsigned grid_1d(int64_t items, int64_t per_block, int64_t most) {
     return (unsigned)std::min(std::max<int64_t>((items + per_block - 1) / per_block, 1), most);
 }
 
+// How a pass lays groups of eight columns over blocks: a block takes `width` groups of `rows` rows (or one
+// row's, in chunks), and every thread keeps its columns while it walks down the rows, so the division that
+// finds them is made once.
+struct RowGrid {
+    int64_t groups;     // of a row
+    int32_t width, rows;
+    int64_t chunks, row_blocks;
+};
+
+RowGrid row_grid(int64_t rows, int64_t F, int64_t most) {
+    RowGrid g;
+    g.groups = (F + 7) / 8;
+    g.width = (int32_t)std::min<int64_t>(g.groups, kRowsBlock);
+    g.rows = kRowsBlock / g.width;
+    g.chunks = (g.groups + g.width - 1) / g.width;
+    g.row_blocks = std::max<int64_t>(1, std::min((rows + g.rows - 1) / g.rows, std::max<int64_t>(1, most / g.chunks)));
+    return g;
+}
+
 // out = res + drop(x), eight columns (two blocks of words) a thread. Bound by memory: one read, one write
 // of each element and the words in between.
 template <int E, bool RES>
 __global__ void __launch_bounds__(kRowsBlock) dropout_kernel(const void *x, int64_t ldx, const void *res, int64_t ldr,
-                                                             int64_t rows, int64_t F, int64_t groups, const Drop d,
+                                                             int64_t rows, int64_t F, const RowGrid grid, const Drop d,
                                                              void *out, int64_t ldo) {
-    const int64_t total = rows * groups, step = (int64_t)gridDim.x * kRowsBlock;
-    for (int64_t i = (int64_t)blockIdx.x * kRowsBlock + threadIdx.x; i < total; i += step) {
-        const int64_t r = i / groups, f = (i - r * groups) * 8, count = F - f;
-        float v[8];
+    const int64_t rb = blockIdx.x / grid.chunks, chunk = blockIdx.x - rb * grid.chunks;
+    const uint32_t row = threadIdx.x / (uint32_t)grid.width, lane = threadIdx.x - row * grid.width;
+    const int64_t f = (chunk * grid.width + lane) * 8, count = F - f;
+    if (row >= (uint32_t)grid.rows || count <= 0) return;
+    for (int64_t r = rb * grid.rows + row; r < rows; r += grid.row_blocks * grid.rows) {
+        float v[8], b[8];
         load_wide<E, 8>(x, r * ldx + f, count, v);
+        if constexpr (RES) load_wide<E, 8>(res, r * ldr + f, count, b);
         if (d.on) {
             drop4(v, (uint32_t)(f >> 2), (uint32_t)r, d);
             drop4(v + 4, (uint32_t)(f >> 2) + 1, (uint32_t)r, d);
         }
         if constexpr (RES) {
-            float b[8];
-            load_wide<E, 8>(res, r * ldr + f, count, b);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += b[j];
         }
@@ -42,36 +62,58 @@ __global__ void __launch_bounds__(kRowsBlock) dropout_kernel(const void *x, int6
     }
 }
 
-// One wave a row: the largest magnitude, then x * (127 / largest) rounded to nearest even. A row that
-// holds NaN or an infinity has no scale: it gets scale NaN and zeros, so that every product of it is NaN.
-// The largest magnitude counts as at least 2^-100, so the factor stays finite.
-template <int E>
+// The low byte of x k, rounded as a product and then to the nearest integer, to even: it is within 127.00002 of
+// 0, where adding 1.5 * 2^23 rounds to integers and leaves them in the low bits. (Product and sum are not
+// fused: that would round once.)
+__device__ __forceinline__ uint32_t nearest(float x, float k) {
+#pragma clang fp contract(off)
+    return __float_as_uint(x * k + 12582912.0f) & 255u;
+}
+
+// L lanes a row (a power of two, up to a wave): the largest magnitude, then x * (127 / largest) rounded to
+// nearest even. Up to NV vectors of eight a lane stay in registers between the two, so the row is read once;
+// longer rows are read again. A row that holds NaN or an infinity has no scale: it gets scale NaN and zeros,
+// so that every product of it is NaN. The largest magnitude counts as at least 2^-100, so the factor
+// stays finite.
+template <int E, int L, int NV>
 __global__ void __launch_bounds__(kRowsBlock) quantize_kernel(const void *x, int64_t ldx, int64_t rows, int64_t F,
                                                               int8_t *q, int64_t ldq, float *scale) {
-    const int lane = threadIdx.x & 63;
-    const int64_t step = (int64_t)gridDim.x * (kRowsBlock / 64);
-    for (int64_t r = (int64_t)blockIdx.x * (kRowsBlock / 64) + (threadIdx.x >> 6); r < rows; r += step) {
+    constexpr int R = kRowsBlock / L;
+    const int lane = threadIdx.x % L;
+    const int64_t step = (int64_t)gridDim.x * R;
+    for (int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / L; r < rows; r += step) {
+        float v[NV][8];
         float top = 0.0f;
-        for (int64_t f = lane * 8; f < F; f += 512) {
-            float v[8];
-            load_wide<E, 8>(x, r * ldx + f, F - f, v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) top = __builtin_elementwise_maximum(top, fabsf(v[j]));
+        for (int i = 0; i < NV; ++i) {
+            const int64_t f = (int64_t)(lane + i * L) * 8;
+            load_wide<E, 8>(x, r * ldx + f, F - f, v[i]);
         }
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, o));
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = __builtin_elementwise_maximum(top, fabsf(v[i][j]));
+        for (int64_t f = (int64_t)(lane + NV * L) * 8; f < F; f += L * 8) {
+            float t[8];
+            load_wide<E, 8>(x, r * ldx + f, F - f, t);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = __builtin_elementwise_maximum(top, fabsf(t[j]));
+        }
+#pragma unroll
+        for (int o = 1; o < L; o <<= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, o));
         const bool finite = top < INFINITY;
         const float a = fmaxf(top, 0x1p-100f), k = 127.0f / a;
         if (lane == 0) scale[r] = finite ? a / 127.0f : NAN;
-        for (int64_t f = lane * 8; f < F; f += 512) {
-            float v[8];
+        auto put = [&](int64_t f, const float *t) {
             const int64_t count = F - f;
-            load_wide<E, 8>(x, r * ldx + f, count, v);
-            uint32_t w[2] = {0, 0};
+            if (count <= 0) return;
+            uint32_t w[2];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int n = finite ? (int)rintf(v[j] * k) : 0;
-                w[j / 4] |= (uint32_t)(n & 255) << (j % 4 * 8);
+            for (int h = 0; h < 2; ++h) {
+                uint32_t b[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) b[j] = finite ? nearest(t[4 * h + j], k) : 0u;
+                w[h] = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
             }
             int8_t *p = q + r * ldq + f;
             typedef uint32_t two __attribute__((ext_vector_type(2), aligned(1)));
@@ -82,28 +124,60 @@ __global__ void __launch_bounds__(kRowsBlock) quantize_kernel(const void *x, int
                 for (int j = 0; j < 8; ++j)
                     if (j < count) p[j] = (int8_t)(w[j / 4] >> (j % 4 * 8));
             }
+        };
+#pragma unroll
+        for (int i = 0; i < NV; ++i) put((int64_t)(lane + i * L) * 8, v[i]);
+        for (int64_t f = (int64_t)(lane + NV * L) * 8; f < F; f += L * 8) {
+            float t[8];
+            load_wide<E, 8>(x, r * ldx + f, F - f, t);
+            put(f, t);
         }
     }
 }
 
-// The parts of a product added in order, then its epilogue: four columns a thread.
-template <int E, int EPI, bool DUAL>
+// The parts of a product added up, then its epilogue. Four columns a thread, or (P > 1) a share of their parts:
+// the eight threads that finish eight runs of four columns sit in one row of a wave and P rows share the
+// parts, which are then added in a fixed order.
+template <int E, int EPI, bool DUAL, int P>
 __global__ void __launch_bounds__(kRowsBlock) join_kernel(const DenseArgs a) {
     typedef typename std::conditional<E == ELEM_I8, int, float>::type Sum;
-    const int64_t groups = (a.N + 3) / 4, total = a.M * groups, step = (int64_t)gridDim.x * kRowsBlock;
+    constexpr int UNITS = P == 1 ? 64 : 64 / P;   // of a wave
+    const int lane = threadIdx.x & 63, share = lane / UNITS;
+    const int64_t groups = (a.N + 3) / 4, total = a.M * groups, step = (int64_t)gridDim.x * (kRowsBlock / P);
     const int64_t C = DUAL ? 2 * a.N : a.N, slab = a.M * C;
-    for (int64_t i = (int64_t)blockIdx.x * kRowsBlock + threadIdx.x; i < total; i += step) {
-        const int64_t m = i / groups, n = (i - m * groups) * 4, count = a.N - n;
+    for (int64_t first = ((int64_t)blockIdx.x * (kRowsBlock / 64) + (threadIdx.x >> 6)) * UNITS; first < total; first += step) {
+        const int64_t i = first + lane % UNITS;
+        const bool in = i < total;
+        const int64_t m = in ? i / groups : 0, n = in ? (i - m * groups) * 4 : 0, count = a.N - n;
         Sum g[4] = {0, 0, 0, 0}, u[4] = {0, 0, 0, 0};
-        const Sum *p = (const Sum *)a.part + m * C + n;
-        for (int s = 0; s < a.splits; ++s, p += slab) {
+        const Sum *p = (const Sum *)a.part + m * C + n + share * slab;
+#pragma unroll 4
+        for (int s = share; s < a.splits; s += P, p += P * slab) {
+            typedef Sum Vec __attribute__((ext_vector_type(4), aligned(4)));
+            if (count >= 4) {
+                const Vec x = *reinterpret_cast<const Vec *>(p);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j < count) {
-                    g[j] += p[j];
-                    if constexpr (DUAL) u[j] += p[a.N + j];
-                }
+                for (int j = 0; j < 4; ++j) g[j] += x[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < count) g[j] += p[j];
+            }
+            if constexpr (DUAL) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < count) u[j] += p[a.N + j];
+            }
         }
+#pragma unroll
+        for (int o = UNITS; o < 64; o <<= 1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                g[j] += __shfl_xor(g[j], o);
+                if constexpr (DUAL) u[j] += __shfl_xor(u[j], o);
+            }
+        }
+        if (!in || share != 0) continue;
         Columns<4> c;
         load_columns<E, EPI, 4>(a, n, c);
         if constexpr (EPI == DENSE_GATED)
@@ -122,12 +196,22 @@ __global__ void __launch_bounds__(kRowsBlock) colsum_mid_kernel(const float *col
     mid[blockIdx.y * C + c] = s;
 }
 
+// The sums of the rows of [rows x 2N]: 16 columns a block, 16 shares of the rows, added in order.
 template <int E>
-__global__ void __launch_bounds__(kRowsBlock) colsum_kernel(const float *mid, int64_t N, void *out0, void *out1) {
-    const int64_t c = (int64_t)blockIdx.x * kRowsBlock + threadIdx.x;
-    if (c >= 2 * N) return;
+__global__ void __launch_bounds__(kRowsBlock) colsum_kernel(const float *sums, int64_t rows, int64_t N, void *out0,
+                                                            void *out1) {
+    __shared__ float part[16][17];
+    const int col = threadIdx.x & 15, share = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + col;
     float s = 0.0f;
-    for (int r = 0; r < kColsumMid; ++r) s += mid[r * 2 * N + c];
+    if (c < 2 * N) {
+#pragma unroll 4
+        for (int64_t r = share; r < rows; r += 16) s += sums[r * 2 * N + c];
+    }
+    part[share][col] = s;
+    __syncthreads();
+    if (share != 0 || c >= 2 * N) return;
+    for (int i = 1; i < 16; ++i) s += part[i][col];
     void *out = c < N ? out0 : out1;
     if (out) store_wide<E, 1>(out, c < N ? c : c - N, 1, &s);
 }
@@ -135,29 +219,47 @@ __global__ void __launch_bounds__(kRowsBlock) colsum_kernel(const float *mid, in
 template <int E>
 hipError_t dropout_of(const void *x, int64_t ldx, const void *res, int64_t ldr, int64_t rows, int64_t F, const Drop &d,
                       void *out, int64_t ldo, hipStream_t st) {
-    const int64_t groups = (F + 7) / 8;
-    const dim3 grid(grid_1d(rows * groups, kRowsBlock, 8192));
+    const RowGrid g = row_grid(rows, F, 16384);
+    if (g.chunks * g.row_blocks > INT32_MAX) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(g.chunks * g.row_blocks));
     if (res)
-        hipLaunchKernelGGL((dropout_kernel<E, true>), grid, dim3(kRowsBlock), 0, st, x, ldx, res, ldr, rows, F, groups, d,
-                           out, ldo);
+        hipLaunchKernelGGL((dropout_kernel<E, true>), grid, dim3(kRowsBlock), 0, st, x, ldx, res, ldr, rows, F, g, d, out,
+                           ldo);
     else
-        hipLaunchKernelGGL((dropout_kernel<E, false>), grid, dim3(kRowsBlock), 0, st, x, ldx, res, ldr, rows, F, groups, d,
-                           out, ldo);
+        hipLaunchKernelGGL((dropout_kernel<E, false>), grid, dim3(kRowsBlock), 0, st, x, ldx, res, ldr, rows, F, g, d, out,
+                           ldo);
     return hipGetLastError();
 }
 
 template <int E>
 hipError_t quantize_of(const void *x, int64_t ldx, int64_t rows, int64_t F, int8_t *q, int64_t ldq, float *scale,
                        hipStream_t st) {
-    hipLaunchKernelGGL(quantize_kernel<E>, dim3(grid_1d(rows, kRowsBlock / 64, 16384)), dim3(kRowsBlock), 0, st, x, ldx,
-                       rows, F, q, ldq, scale);
-    return hipGetLastError();
+    const int64_t groups = (F + 7) / 8;
+    auto run = [&](auto lanes, auto vectors) {
+        constexpr int L = decltype(lanes)::value, NV = decltype(vectors)::value;
+        hipLaunchKernelGGL((quantize_kernel<E, L, NV>), dim3(grid_1d(rows, kRowsBlock / L, 16384)), dim3(kRowsBlock), 0, st,
+                           x, ldx, rows, F, q, ldq, scale);
+        return hipGetLastError();
+    };
+    typedef std::integral_constant<int, 1> One;
+    typedef std::integral_constant<int, 64> Wave;
+    if (groups <= 4) return run(std::integral_constant<int, 4>(), One());
+    if (groups <= 16) return run(std::integral_constant<int, 16>(), One());
+    if (groups <= 64) return run(Wave(), One());
+    if (groups <= 128) return run(Wave(), std::integral_constant<int, 2>());
+    if (groups <= 256) return run(Wave(), std::integral_constant<int, 4>());
+    return run(Wave(), std::integral_constant<int, 8>());
 }
 
 template <int E, int EPI, bool DUAL>
 hipError_t join_of(const DenseArgs &a, hipStream_t st) {
-    hipLaunchKernelGGL((join_kernel<E, EPI, DUAL>), dim3(grid_1d(a.M * ((a.N + 3) / 4), kRowsBlock, 16384)),
-                       dim3(kRowsBlock), 0, st, a);
+    const int64_t units = a.M * ((a.N + 3) / 4);
+    if (a.splits >= 8)
+        hipLaunchKernelGGL((join_kernel<E, EPI, DUAL, 8>), dim3(grid_1d(units, kRowsBlock / 8, 16384)), dim3(kRowsBlock), 0,
+                           st, a);
+    else
+        hipLaunchKernelGGL((join_kernel<E, EPI, DUAL, 1>), dim3(grid_1d(units, kRowsBlock, 16384)), dim3(kRowsBlock), 0, st,
+                           a);
     return hipGetLastError();
 }
 
@@ -169,8 +271,9 @@ hipError_t join_float(int epi, const DenseArgs &a, hipStream_t st) {
 }
 
 template <int E>
-hipError_t colsum_of(const float *mid, int64_t N, unsigned gx, void *out0, void *out1, hipStream_t st) {
-    hipLaunchKernelGGL(colsum_kernel<E>, dim3(gx), dim3(kRowsBlock), 0, st, mid, N, out0, out1);
+hipError_t colsum_of(const float *sums, int64_t rows, int64_t N, void *out0, void *out1, hipStream_t st) {
+    hipLaunchKernelGGL(colsum_kernel<E>, dim3((unsigned)((2 * N + 15) / 16)), dim3(kRowsBlock), 0, st, sums, rows, N, out0,
+                       out1);
     return hipGetLastError();
 }
 
@@ -202,14 +305,19 @@ hipError_t launch_dense_join(int elem, int epi, const DenseArgs &a, hipStream_t 
 
 hipError_t launch_colsum(int elem, const float *colsum, int64_t rows, int64_t N, float *mid, void *out0, void *out1,
                          hipStream_t st) {
-    const unsigned gx = (unsigned)((2 * N + kRowsBlock - 1) / kRowsBlock);
-    hipLaunchKernelGGL(colsum_mid_kernel, dim3(gx, (unsigned)kColsumMid), dim3(kRowsBlock), 0, st, colsum, rows, 2 * N,
-                       mid);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (elem == ELEM_F32) return colsum_of<ELEM_F32>(mid, N, gx, out0, out1, st);
-    if (elem == ELEM_BF16) return colsum_of<ELEM_BF16>(mid, N, gx, out0, out1, st);
-    return colsum_of<ELEM_F16>(mid, N, gx, out0, out1, st);
+    // many rows: down to kColsumMid first
+    if (rows > 16 * kColsumMid) {
+        const unsigned gx = (unsigned)((2 * N + kRowsBlock - 1) / kRowsBlock);
+        hipLaunchKernelGGL(colsum_mid_kernel, dim3(gx, (unsigned)kColsumMid), dim3(kRowsBlock), 0, st, colsum, rows, 2 * N,
+                           mid);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        colsum = mid;
+        rows = kColsumMid;
+    }
+    if (elem == ELEM_F32) return colsum_of<ELEM_F32>(colsum, rows, N, out0, out1, st);
+    if (elem == ELEM_BF16) return colsum_of<ELEM_BF16>(colsum, rows, N, out0, out1, st);
+    return colsum_of<ELEM_F16>(colsum, rows, N, out0, out1, st);
 }
 
 }  // namespace geot

@@ -52,44 +52,50 @@ __global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs
 
     const int64_t kbytes = a.K * ES, whole = kbytes / 64;
     const bool narrow = kbytes < 16;
-    auto steps = [&](auto count, int64_t s) {
+    // C of the wave's steps from s, all loaded before the first is multiplied. With MASK steps from `whole`
+    // on do not exist: the last one is loaded in their place and not multiplied.
+    auto steps = [&](auto count, auto mask, int64_t s) {
         constexpr int C = decltype(count)::value;
+        constexpr bool MASK = decltype(mask)::value;
         chunk_t x[C][FM], w[C][FN];
 #pragma unroll
         for (int u = 0; u < C; ++u) {
-            const int64_t at = (s + kSmallWaves * u) * 64;
+            const int64_t st = s + kSmallWaves * u, at = (MASK && st >= whole ? whole - 1 : st) * 64;
 #pragma unroll
             for (int j = 0; j < FN; ++j) w[u][j] = *reinterpret_cast<const chunk_any *>(pw[j] + at);
 #pragma unroll
             for (int i = 0; i < FM; ++i) x[u][i] = *reinterpret_cast<const chunk_any *>(px[i] + at);
         }
 #pragma unroll
-        for (int u = 0; u < C; ++u)
+        for (int u = 0; u < C; ++u) {
+            if (MASK && s + kSmallWaves * u >= whole) break;
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
                 for (int j = 0; j < FN; ++j) acc[i][j] = mma<E>(w[u][j], x[u][i], acc[i][j]);
+        }
     };
-    int64_t s = wave;
-    for (; s + kSmallWaves * (U - 1) < whole; s += kSmallWaves * U) steps(std::integral_constant<int, U>(), s);
-    if (s + kSmallWaves < whole) {
-        for (; s + kSmallWaves < whole; s += 2 * kSmallWaves) steps(std::integral_constant<int, 2>(), s);
-    }
-    if (s < whole) {
-        steps(std::integral_constant<int, 1>(), s);
-        s += kSmallWaves;
-    }
-    if (s == whole && whole * 64 < kbytes) {   // the step that K cuts short, in the wave whose turn it is
+    typedef std::integral_constant<int, U> Full;
+    typedef std::integral_constant<int, U / 2> Half;
+    // the step that K cuts short is the wave's whose turn it is; its loads go first
+    const bool mine = whole % kSmallWaves == wave && whole * 64 < kbytes;
+    chunk_t xs[FM], ws[FN];
+    if (mine) {
         const int64_t left = kbytes - whole * 64 - c4 * 16;
-        chunk_t x[FM], w[FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j) w[j] = load_chunk<ES>(pw[j] + whole * 64, left, narrow);
+        for (int j = 0; j < FN; ++j) ws[j] = load_chunk<ES>(pw[j] + whole * 64, left, narrow);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) x[i] = load_chunk<ES>(px[i] + whole * 64, left, narrow);
+        for (int i = 0; i < FM; ++i) xs[i] = load_chunk<ES>(px[i] + whole * 64, left, narrow);
+    }
+    int64_t s = wave;
+    for (; s + kSmallWaves * (U - 1) < whole; s += kSmallWaves * U) steps(Full(), std::false_type(), s);
+    if (s + kSmallWaves * (U / 2) < whole) steps(Full(), std::true_type(), s);
+    else if (s < whole) steps(Half(), std::true_type(), s);
+    if (mine) {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = mma<E>(w[j], x[i], acc[i][j]);
+            for (int j = 0; j < FN; ++j) acc[i][j] = mma<E>(ws[j], xs[i], acc[i][j]);
     }
 
 #pragma unroll

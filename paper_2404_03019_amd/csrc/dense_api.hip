@@ -138,8 +138,8 @@ DensePlan plan_dense(int elem, int epi, int mode, int64_t M, int64_t N, int64_t 
     p.tiles_m = up(M, tile);
     p.tiles_n = up(N, dual ? tile / 2 : tile);
     const int64_t tiles = std::max<int64_t>(1, p.tiles_m * p.tiles_n);
-    p.steps_per = std::max<int64_t>(steps, 1);
-    if (epi != DENSE_GATED_BWD && tiles < kDenseCUs && steps > 1) {
+    p.steps_per = (int64_t)1 << 40;   // all of them
+    if (p.tile == DENSE_TILE_128 && epi != DENSE_GATED_BWD && tiles < kDenseCUs && steps > 1) {
         const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2 * kDenseCUs / tiles, steps / 2));
         p.steps_per = up(up(steps, want), 2) * 2;   // even: the kernel takes steps in pairs
         p.splits = up(steps, p.steps_per);
@@ -307,11 +307,12 @@ geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stri
 
         // dG and dU side by side in the storage type, [M x Np] each: the rounding that the gradients of two
         // separate projections would have. Each starts on 16 bytes in every row.
-        const int64_t lane = 16 / es, Np = up(N, lane) * lane, ld2 = 2 * Np;
+        const int64_t lane = 16 / es, Np = up(N, lane) * lane;
+        const int64_t ld2 = 2 * Np + (2 * Np * es % 2048 == 0 ? 128 / es : 0);   // rows not all on one memory channel
         const DensePlan p0 = plan_dense(elem, DENSE_GATED_BWD, DENSE_NT, M, N, K, true, 1, gated_direct(q));
         const DensePlan px = plan_dense(elem, DENSE_PLAIN, DENSE_NN, M, K, N, false, 2,
                                         direct_ok(w_gate, w_stride, es, K) && direct_ok(w_up, w_stride, es, K) && ld2 * es < ((int64_t)1 << 23));
-        const DensePlan pw = plan_dense(elem, DENSE_PLAIN, DENSE_TN, ld2, K, M, false, 1,
+        const DensePlan pw = plan_dense(elem, DENSE_PLAIN, DENSE_TN, 2 * Np, K, M, false, 1,
                                         direct_ok(x, x_stride, es, K) && ld2 * es < ((int64_t)1 << 23));
         size_t at = 0;
         auto take = [&](size_t b) {
@@ -374,7 +375,7 @@ geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stri
             a.lda = ld2;
             a.b0 = x;
             a.ldb = x_stride;
-            a.M = ld2;
+            a.M = 2 * Np;
             a.N = K;
             a.K = M;
             a.out = grad_w_gate;

@@ -45,6 +45,7 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t chunk_any __attribute__((ext_vector_type(4), aligned(1)));
 typedef uint32_t chunk_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) const char lds_char;
 typedef __attribute__((address_space(1))) const void global_void;
 
 constexpr int kStepBytes = 128;
@@ -162,37 +163,54 @@ struct Tile {
             if constexpr (NV > 4) return (row & 3) | (((row / NV) & 1) << 2);
             else return row & 7;
         } else if constexpr (ES == 2) {
-            return (row & 3) << 1;
+            // a transposing read takes four rows from each of several runs of eight in one cycle
+            return ((row & 3) << 1) | ((((row >> 3) ^ (row >> 4)) & 1) << 3);
         } else {
-            return ((row >> 2) & 1) << 2;
+            return ((row >> 2) & 3) << 2;
         }
     }
     // chunk i: its row of LDS, and the chunk of that row in memory that it holds
     static __device__ __forceinline__ int row_of(int i) { return i / CPR; }
     static __device__ __forceinline__ int chunk_of(int i) { return (i % CPR) ^ key(i / CPR); }
 
-    // fragment: the operand of one matrix instruction for 16 rows (columns) from `first`, half kk of the
-    // step. With dealt columns `first` already holds the lane's own row.
-    static __device__ __forceinline__ chunk_t fragment(const char *lds, int row, int kk, int r16, int c4) {
+    // Fragment: the operand of one matrix instruction for 16 rows (columns) of the tile, half kk of the step.
+    // `at` places it: the lane's own row, or (row per k) the byte where its column of half 0 stands, the
+    // same for both halves but for a constant.
+    static __device__ __forceinline__ int place(int start, int row, int r16, int c4) {
         if constexpr (!KMAJOR) {
-            return *reinterpret_cast<const chunk_t *>(lds + row * kStepBytes + (((4 * kk + c4) ^ key(row)) << 4));
+            return row;
+        } else {
+            int p;
+            if constexpr (ES == 2) {   // the lane reads four columns of row k (k and k + 4 have one key)
+                const int k = 8 * c4 + (r16 >> 2), byte = (row + 4 * (r16 & 3)) * 2;
+                p = start + k * ROW + (((byte >> 4) ^ key(k)) << 4) + (byte & 15);
+            } else {
+                const int k = 4 * c4, byte = (row + r16) * 4;
+                p = start + k * ROW + (((byte >> 4) ^ key(k)) << 4) + (byte & 15);
+            }
+            // one opaque number: taken apart into many small sums, the addresses lose their connection with
+            // the LDS array and every read would wait for all loads on their way
+            asm("" : "+v"(p));
+            return p;
+        }
+    }
+    static __device__ __forceinline__ chunk_t fragment(lds_char *lds, int start, int at, int kk, int c4) {
+        if constexpr (!KMAJOR) {
+            typedef __attribute__((address_space(3))) const chunk_t lds_chunk;
+            return *(lds_chunk *)(lds + (start + at * kStepBytes + (((4 * kk + c4) ^ key(at)) << 4)));
         } else if constexpr (ES == 2) {
-            const int k = 32 * kk + 8 * c4 + (r16 >> 2), at = (row + 4 * (r16 & 3)) * 2;
-            typedef __attribute__((address_space(3))) i16x4 lds4;
-            const int p = k * ROW + (((at >> 4) ^ key(k)) << 4) + (at & 15);   // rows k and k + 4 have one key
-            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(lds + p));
-            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(lds + p + 4 * ROW));
+            typedef __attribute__((address_space(3))) i16x4 lds_4;
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_4 *)(lds + (at + 32 * kk * ROW)));
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_4 *)(lds + (at + (32 * kk + 4) * ROW)));
             chunk_t v;
             v.xy = __builtin_bit_cast(half_t, lo);
             v.zw = __builtin_bit_cast(half_t, hi);
             return v;
         } else {
+            typedef __attribute__((address_space(3))) const uint32_t lds_word;
             chunk_t v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = 16 * kk + 4 * c4 + j, at = (row + r16) * 4;
-                v[j] = *reinterpret_cast<const uint32_t *>(lds + k * ROW + (((at >> 4) ^ key(k)) << 4) + (at & 15));
-            }
+            for (int j = 0; j < 4; ++j) v[j] = *(lds_word *)(lds + (at + (16 * kk + j) * ROW));   // one key for all
             return v;
         }
     }
@@ -337,11 +355,14 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
 
     // the lane's row of A and columns of B in LDS
     const int arow = wm * (BM / WM) + (KA ? 0 : r16);
-    int brow[FN];
+    int brow[FN], acol[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) acol[i] = KA ? TA::place(0, arow + 16 * i, r16, c4) : 0;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const int f = j % PF;
-        brow[j] = (j / PF) * HB + wn * (16 * PF) + (KB ? 16 * f : 4 * PF * (r16 >> 2) + 4 * f + (r16 & 3));
+        brow[j] = TB::place(BM * kStepBytes, (j / PF) * HB + wn * (16 * PF) + (KB ? 16 * f : 4 * PF * (r16 >> 2) + 4 * f + (r16 & 3)),
+                            r16, c4);
     }
     Acc acc[FM][FN];
 
@@ -350,11 +371,11 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
     };
     constexpr int kAccRegs = FM * FN * 4;
     constexpr bool PINNED = kAccRegs >= 256;
-    auto read_w = [&](Frags &f, const char *lds, int kk, int j) {
-        f.w[j] = TB::fragment(lds + BM * kStepBytes, brow[j], kk, r16, c4);
+    auto read_w = [&](Frags &f, lds_char *lds, int kk, int j) {
+        f.w[j] = TB::fragment(lds, BM * kStepBytes, brow[j], kk, c4);
     };
-    auto read_x = [&](Frags &f, const char *lds, int kk, int i) {
-        f.x[i] = TA::fragment(lds, arow + 16 * i, kk, r16, c4);
+    auto read_x = [&](Frags &f, lds_char *lds, int kk, int i) {
+        f.x[i] = TA::fragment(lds, 0, KA ? acol[i] : arow + 16 * i, kk, c4);
     };
     auto multiply = [&](const Frags &f, int i) {
 #pragma unroll
@@ -366,6 +387,7 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
     // Between two turns no wave writes what another reads: before one, every load into LDS has landed
     // (vmcnt 0 counts them) and every read of the buffer that is written next is done.
     auto turn = [&]() {
+        __builtin_amdgcn_sched_barrier(0);   // the wait stays here, behind the multiplications
         __builtin_amdgcn_s_waitcnt(0x0f70);
         __syncthreads();
     };
@@ -398,7 +420,7 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
         // One wave a SIMD: the next half's operands are read while this one's are multiplied, in this order:
         // those that the next half needs first come first.
         Frags f0, f1;
-        auto read_part = [&](Frags &next, const char *lds, int kk, int i) {
+        auto read_part = [&](Frags &next, lds_char *lds, int kk, int i) {
 #pragma unroll
             for (int r = i * (FN + FM) / FM; r < (i + 1) * (FN + FM) / FM; ++r) {
                 if (r < FN) read_w(next, lds, kk, r);
@@ -406,7 +428,7 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
             }
             __builtin_amdgcn_sched_barrier(0);
         };
-        auto phase = [&](const Frags &now, Frags &next, const char *lds, int kk) {
+        auto phase = [&](const Frags &now, Frags &next, lds_char *lds, int kk) {
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
                 read_part(next, lds, kk, i);
@@ -415,10 +437,10 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
             }
         };
 #pragma unroll
-        for (int i = 0; i < FM; ++i) read_part(f0, lds0, 0, i);
+        for (int i = 0; i < FM; ++i) read_part(f0, (lds_char *)lds0, 0, i);
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            read_part(f1, lds0, 1, i);
+            read_part(f1, (lds_char *)lds0, 1, i);
 #pragma unroll
             for (int j = 0; j < FN; ++j) mma_first<E>(f0.w[j], f0.x[i], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
@@ -426,16 +448,16 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
         for (int64_t j = 2; j < slots; j += 2) {
             turn();
             issue(lds0, j);
-            phase(f1, f0, lds1, 0);
-            phase(f0, f1, lds1, 1);
+            phase(f1, f0, (lds_char *)lds1, 0);
+            phase(f0, f1, (lds_char *)lds1, 1);
             turn();
             issue(lds1, j + 1);
-            phase(f1, f0, lds0, 0);
-            phase(f0, f1, lds0, 1);
+            phase(f1, f0, (lds_char *)lds0, 0);
+            phase(f0, f1, (lds_char *)lds0, 1);
         }
         turn();
-        phase(f1, f0, lds1, 0);
-        phase(f0, f1, lds1, 1);
+        phase(f1, f0, (lds_char *)lds1, 0);
+        phase(f0, f1, (lds_char *)lds1, 1);
 #pragma unroll
         for (int i = 0; i < FM; ++i) multiply(f1, i);
         settle();
@@ -449,7 +471,7 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
         Frags f;
-        auto product = [&](const char *lds) {
+        auto product = [&](lds_char *lds) {
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
 #pragma unroll
@@ -460,18 +482,19 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
                 for (int i = 0; i < FM; ++i) multiply(f, i);
             }
         };
-        for (int64_t j = 2;; j += 2) {
-            product(lds0);
+        product((lds_char *)lds0);
+        for (int64_t j = 2; j < slots; j += 2) {
             turn();
-            const bool more = j < slots;
-            if (more) issue(lds0, j);
-            product(lds1);
-            if (!more) break;
+            issue(lds0, j);
+            product((lds_char *)lds1);
             land(lds0);
             turn();
             issue(lds1, j + 1);
+            product((lds_char *)lds0);
             land(lds1);
         }
+        turn();
+        product((lds_char *)lds1);
     }
     epilogue<E, EPI, FM, FN, PF, DUAL, KB ? 4 : 4 * PF>(a, split, m0 + wm * (BM / WM) + r16,
                                                         n0 + wn * (16 * PF) + (KB ? 4 : 4 * PF) * c4, acc,

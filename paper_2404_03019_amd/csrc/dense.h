@@ -32,8 +32,9 @@ enum DenseMode : int {
     DENSE_TN = 2,  // both have a row per k
 };
 
-// DENSE_TILE_SMALL: blocks of 16 fm rows and 16 fn weight rows, whose waves share K
-enum DenseTile : int { DENSE_TILE_128 = 0, DENSE_TILE_256 = 1, DENSE_TILE_SMALL = 2 };
+// DENSE_TILE_SMALL: blocks of 16 fm rows and 16 fn weight rows, whose waves share K. DENSE_TILE_NARROW: rows of
+// up to 64 fm bytes, fn waves over the columns; a block goes on to further rows.
+enum DenseTile : int { DENSE_TILE_128 = 0, DENSE_TILE_256 = 1, DENSE_TILE_SMALL = 2, DENSE_TILE_NARROW = 3 };
 
 // C[m, n] = sum_k A[m, k] B[n, k]. With DENSE_NT and b1 there are two column operands: g comes from b0 and u
 // from b1, N columns each. With DENSE_NN and b1 K comes twice: A's second K columns start seg_a bytes
@@ -64,7 +65,8 @@ struct DenseArgs {
 // Tile and split of a product, chosen by plan_dense from its sizes.
 struct DensePlan {
     int tile;         // DenseTile
-    int fm, fn;       // DENSE_TILE_SMALL
+    int fm, fn;       // DENSE_TILE_SMALL and DENSE_TILE_NARROW
+    int64_t blocks;   // DENSE_TILE_NARROW
     bool direct;      // whole steps are loaded straight into LDS
     int64_t splits;   // parts of K; more than one takes `part` and a join
     int64_t steps_per;

@@ -112,7 +112,7 @@ static bool direct_ok(const void *p, int64_t ld, int64_t es, int64_t cols = 0) {
 }
 
 DensePlan plan_dense(int elem, int epi, int mode, int64_t M, int64_t N, int64_t K, bool dual, int segments, bool direct) {
-    DensePlan p{DENSE_TILE_128, 0, 0, direct, 1, 0, 0, 0, 0, 0};
+    DensePlan p{DENSE_TILE_128, 0, 0, 0, direct, 1, 0, 0, 0, 0, 0};
     const int64_t steps = K * elem_bytes(elem) / 128 * segments, C = dual ? 2 * N : N;   // whole steps
     // 256 x 256 tiles (one block a CU) take a step in 1.6 us and 7 us besides, 128 x 128 ones (two a CU) 1.0
     // and 3; whichever gets through its rounds sooner. Measured, gated block, bf16, 256 / 128: 16,384 rows,
@@ -129,6 +129,19 @@ DensePlan plan_dense(int elem, int epi, int mode, int64_t M, int64_t N, int64_t 
         p.fn = p.tiles_m * up(C, 64) >= kDenseCUs ? 4 : dual ? 2 : 1;
         p.tiles_n = up(N, dual ? 8 * p.fn : 16 * p.fn);
         p.colsum_rows = p.tiles_m * p.fm;
+        return p;
+    }
+    const int64_t kbytes = K * elem_bytes(elem);
+    if (dual && kbytes <= 512) {
+        // Narrow rows: a block for every CU, each with a panel of columns.
+        p.tile = DENSE_TILE_NARROW;
+        p.fm = kbytes <= 128 ? 2 : kbytes <= 256 ? 4 : 8;
+        p.fn = p.fm < 8 && N <= 128 ? 4 : 8;
+        p.tiles_m = up(M, 64);
+        p.tiles_n = up(N, (p.fm < 8 ? 32 : 16) * p.fn);
+        const int64_t each = std::max<int64_t>(1, std::min(up(p.tiles_m, 8), kDenseCUs / 8 / std::min(p.tiles_n, kDenseCUs / 8)));
+        p.blocks = 8 * p.tiles_n * each;
+        p.colsum_rows = 8 * each * (8 / p.fn);
         return p;
     }
     if (direct && elem != ELEM_F32 && t_big >= kDenseCUs &&
@@ -155,7 +168,7 @@ hipError_t launch_dense(int elem, int epi, int mode, DenseArgs a, const DensePla
     a.tiles_n = plan.tiles_n;
     a.splits = (int32_t)plan.splits;
     a.steps_per = plan.steps_per;
-    const int64_t blocks = a.tiles_m * a.tiles_n * plan.splits;
+    const int64_t blocks = plan.tile == DENSE_TILE_NARROW ? plan.blocks : a.tiles_m * a.tiles_n * plan.splits;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const int e = plan.splits > 1 ? DENSE_PART : epi;
     hipError_t r = hipErrorInvalidValue;

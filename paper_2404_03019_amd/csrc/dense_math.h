@@ -197,10 +197,11 @@ __device__ __forceinline__ void load_columns(const DenseArgs &a, int64_t n, Colu
 }
 
 // Row m, columns n .. n + NV (as many as there are: at least one) of the product. g, u: the sums on entry;
-// DENSE_GATED_BWD leaves dG, dU there (0 beyond the last column).
+// DENSE_GATED_BWD takes the incoming gradient in y (0 beyond the last column) and leaves dG, dU in g and u (0
+// there as well).
 template <int E, int EPI, int ACT, int NV, bool DUAL, class Sum>
 __device__ __forceinline__ void finish(const DenseArgs &a, int64_t split, int64_t m, int64_t n, const Columns<NV> &c,
-                                       Sum *g, Sum *u) {
+                                       Sum *g, Sum *u, float *y) {
     const int64_t count = a.N - n;
     if constexpr (EPI == DENSE_PART) {
         const int64_t C = DUAL ? 2 * a.N : a.N;
@@ -214,7 +215,6 @@ __device__ __forceinline__ void finish(const DenseArgs &a, int64_t split, int64_
         if (!a.out1 || row < a.rows1)
             store_wide<E, NV>(second ? a.out1 : a.out, row * a.ldo + n, count, (const float *)g);
     } else if constexpr (EPI == DENSE_I8) {
-        float y[NV];
         const float sx = a.sx[m];
 #pragma unroll
         for (int v = 0; v < NV; ++v) y[v] = (float)g[v] * sx * c.p[v] + c.q[v];
@@ -222,7 +222,7 @@ __device__ __forceinline__ void finish(const DenseArgs &a, int64_t split, int64_
         else if (a.out_elem == ELEM_F16) store_wide<ELEM_F16, NV>(a.out, m * a.ldo + n, count, y);
         else store_wide<ELEM_F32, NV>(a.out, m * a.ldo + n, count, y);
     } else if constexpr (EPI == DENSE_GATED) {
-        float y[NV], d;
+        float d;
 #pragma unroll
         for (int v = 0; v < NV; ++v) y[v] = activate<E, ACT>(g[v] + c.p[v], &d) * (u[v] + c.q[v]);
         if (a.drop.on) {
@@ -231,8 +231,6 @@ __device__ __forceinline__ void finish(const DenseArgs &a, int64_t split, int64_
         }
         store_wide<E, NV>(a.out, m * a.ldo + n, count, y);
     } else {
-        float y[NV];
-        load_wide<E, NV>(a.grad, m * a.ldg + n, count, y);   // 0 beyond the last column
         if (a.drop.on) {
 #pragma unroll
             for (int v = 0; v < NV; v += 4) drop4(y + v, (uint32_t)((n + v) >> 2), (uint32_t)m, a.drop);
@@ -247,6 +245,26 @@ __device__ __forceinline__ void finish(const DenseArgs &a, int64_t split, int64_
         }
         store_wide<E, NV>(a.out, m * a.ldo + n, count, g);
         store_wide<E, NV>(a.out1, m * a.ldo + n, count, u);
+    }
+}
+
+// The sums over rows that a lane has made of dG and dU, added over the 16 lanes that hold the same columns, to row
+// csrow of `colsum`.
+template <int NV>
+__device__ __forceinline__ void store_colsum(const DenseArgs &a, int64_t csrow, int64_t n, float *csg, float *csu, int r16) {
+    if (!a.colsum) return;
+    float *dst = a.colsum + csrow * 2 * a.N;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) {
+            csg[v] += __shfl_xor(csg[v], o);
+            csu[v] += __shfl_xor(csu[v], o);
+        }
+        if (r16 == 0 && n + v < a.N) {
+            dst[n + v] = csg[v];
+            dst[a.N + n + v] = csu[v];
+        }
     }
 }
 
@@ -271,12 +289,15 @@ __device__ __forceinline__ void epilogue(const DenseArgs &a, int64_t split, int6
             for (int i = 0; i < FM; ++i) {
                 if (m + 16 * i < a.M && nj < a.N) {
                     Sum g[NV], u[NV];
+                    float y[NV];
 #pragma unroll
                     for (int v = 0; v < NV; ++v) {
                         g[v] = acc[i][j + v / 4][v % 4];
                         if constexpr (DUAL) u[v] = acc[i][PF + j + v / 4][v % 4];
                     }
-                    finish<E, EPI, ACT, NV, DUAL>(a, split, m + 16 * i, nj, c, g, u);
+                    if constexpr (EPI == DENSE_GATED_BWD)
+                        load_wide<E, NV>(a.grad, (m + 16 * i) * a.ldg + nj, a.N - nj, y);
+                    finish<E, EPI, ACT, NV, DUAL>(a, split, m + 16 * i, nj, c, g, u, y);
                     if constexpr (EPI == DENSE_GATED_BWD) {
 #pragma unroll
                         for (int v = 0; v < NV; ++v) {
@@ -286,23 +307,7 @@ __device__ __forceinline__ void epilogue(const DenseArgs &a, int64_t split, int6
                     }
                 }
             }
-            if constexpr (EPI == DENSE_GATED_BWD) {
-                if (a.colsum) {
-                    float *dst = a.colsum + csrow * 2 * a.N;
-#pragma unroll
-                    for (int v = 0; v < NV; ++v) {
-#pragma unroll
-                        for (int o = 1; o < 16; o <<= 1) {
-                            csg[v] += __shfl_xor(csg[v], o);
-                            csu[v] += __shfl_xor(csu[v], o);
-                        }
-                        if (r16 == 0 && nj + v < a.N) {
-                            dst[nj + v] = csg[v];
-                            dst[a.N + nj + v] = csu[v];
-                        }
-                    }
-                }
-            }
+            if constexpr (EPI == DENSE_GATED_BWD) store_colsum<NV>(a, csrow, nj, csg, csu, r16);
         };
         if constexpr (EPI == DENSE_GATED || EPI == DENSE_GATED_BWD) with_act(a.act, rows);
         else rows(std::integral_constant<int, ACT_NONE>());

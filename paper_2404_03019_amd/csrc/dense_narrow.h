@@ -1,0 +1,156 @@
+// The gated block's products where the input is narrow (a node's features: up to 512 bytes a row) and the rows
+// are many.
+//
+// Such a product is bound by reading x and writing the result, and a tile's own start and end (its loads, the
+// activations, its stores) outlast its few steps of K. So a block stays: each wave keeps 16 PF columns of
+// both weight matrices in registers, whole, and walks down the rows. While a tile of rows is multiplied
+// and finished the next one is on its way to registers and from there into the other of two LDS buffers;
+// one barrier a tile. The gradients' pass loads its tile of the incoming gradient before it multiplies, and
+// keeps the bias gradients' sums in registers to the end.
+#pragma once
+
+#include "dense_kernel.h"
+
+namespace geot {
+namespace {
+
+// KC: 64-byte pieces of a row; WN waves share the columns, 8 / WN the 64 rows of a tile. Up to 256 bytes a wave
+// has 32 columns of each operand (64 registers of weights at the most), to 512 bytes 16.
+template <int E, int KC, int WN, int EPI>
+__global__ void __launch_bounds__(512) narrow_kernel(const DenseArgs a, const int panels) {
+    constexpr int ES = E == ELEM_F32 ? 4 : 2;
+    constexpr int PF = KC <= 4 ? 2 : 1, FN = 2 * PF, NV = 4 * PF;
+    constexpr int WM = 8 / WN, RT = 64, FM = RT / WM / 16, ROW = KC * 64;
+    constexpr int C = RT * KC * 4 / 512;              // chunks a thread stages
+    static_assert(C >= 1 && RT * KC * 4 % 512 == 0, "whole chunks");
+    typedef typename AccOf<E>::type Acc;
+    __shared__ __align__(16) char lds[2][RT * ROW];
+
+    // blocks of one chiplet take the panels of columns in turn, and then the next tile of rows: the panels'
+    // reads of x meet in its L2
+    const int x8 = blockIdx.x & 7, i8 = blockIdx.x >> 3;
+    const int panel = i8 % panels;
+    const int64_t tile0 = (int64_t)(i8 / panels) * 8 + x8, stride = (int64_t)(gridDim.x / 8 / panels) * 8;
+    const int64_t tiles = (a.M + RT - 1) / RT;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wn = wave % WN, wm = wave / WN, r16 = lane & 15, c4 = lane >> 4;
+    const int64_t n0 = (int64_t)panel * (16 * PF * WN) + wn * 16 * PF, n = n0 + NV * c4;
+    const int64_t kbytes = a.K * ES;
+    const bool narrow = kbytes < 16;
+    auto key = [](int row) { return KC == 1 ? (row >> 1) & 3 : row & 7; };
+
+    // the wave's weights: columns dealt so that a lane's results are 8 next to each other
+    chunk_t w[KC][FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int64_t col = n0 + NV * (r16 >> 2) + 4 * (j % PF) + (r16 & 3);
+        const char *p = (const char *)(j < PF ? a.b0 : a.b1) + (col < a.N ? col : a.N - 1) * a.ldb * ES;
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+            const int64_t at = k * 64 + c4 * 16;
+            w[k][j] = load_chunk<ES>(p + at, kbytes - at, narrow);
+        }
+    }
+    Columns<NV> cols;
+    load_columns<E, EPI, NV>(a, n, cols);
+    float csg[NV], csu[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) csg[v] = csu[v] = 0.0f;
+
+    chunk_t stage[C];
+    auto fetch = [&](int64_t tile) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int i = tid + c * 512, row = i / (KC * 4), at = (i % (KC * 4)) * 16;
+            const int64_t m = tile * RT + row;
+            stage[c] = load_chunk<ES>((const char *)a.a + (m < a.M ? m : a.M - 1) * a.lda * ES + at, kbytes - at, narrow);
+        }
+    };
+    auto land = [&](int buf) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int i = tid + c * 512, row = i / (KC * 4), at = i % (KC * 4);
+            *reinterpret_cast<chunk_t *>(&lds[buf][row * ROW + ((at ^ key(row)) << 4)]) = stage[c];
+        }
+    };
+    typedef typename StoreOf<E>::type T;
+    constexpr int GV = E == ELEM_F32 ? 4 : NV, GW = NV / GV;   // vectors of the lane's columns
+    typedef typename Pack<E, GV>::type Wide;
+
+    if (tile0 < tiles) fetch(tile0);
+    with_act(a.act, [&](auto act) {
+        int buf = 0;
+        for (int64_t tile = tile0; tile < tiles; tile += stride, buf ^= 1) {
+            land(buf);
+            if (tile + stride < tiles) fetch(tile + stride);
+            const int64_t m = tile * RT + wm * 16 * FM + r16;
+            const bool whole = n + NV <= a.N;
+            Wide grad[EPI == DENSE_GATED_BWD ? FM : 1][GW];
+            if constexpr (EPI == DENSE_GATED_BWD) {
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+                    if (whole && m + 16 * i < a.M) {
+                        const T *p = (const T *)a.grad + (m + 16 * i) * a.ldg + n;
+#pragma unroll
+                        for (int h = 0; h < GW; ++h) grad[i][h] = *reinterpret_cast<const Wide *>(p + h * GV);
+                    }
+            }
+            __syncthreads();   // the tile is in LDS; the other buffer has been read
+            // 16 rows at a time, from the first multiplication to the store: few sums are held, and one wave's
+            // multiplications run beside the other's activations
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int row = wm * 16 * FM + 16 * i + r16;
+                Acc acc[FN];
+#pragma unroll
+                for (int k = 0; k < KC; ++k) {
+                    const chunk_t x = *reinterpret_cast<const chunk_t *>(&lds[buf][row * ROW + (((4 * k + c4) ^ key(row)) << 4)]);
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[j] = mma<E>(w[k][j], x, k ? acc[j] : Acc{0, 0, 0, 0});
+                }
+                if (n < a.N && m + 16 * i < a.M) {
+                    float g[NV], u[NV], y[NV];
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) {
+                        g[v] = acc[v / 4][v % 4];
+                        u[v] = acc[PF + v / 4][v % 4];
+                    }
+                    if constexpr (EPI == DENSE_GATED_BWD) {
+                        if (whole) {
+#pragma unroll
+                            for (int v = 0; v < NV; ++v) y[v] = (float)grad[i][v / GV][v % GV];
+                        } else {
+                            load_wide<E, NV>(a.grad, (m + 16 * i) * a.ldg + n, a.N - n, y);
+                        }
+                    }
+                    finish<E, EPI, decltype(act)::value, NV, true>(a, 0, m + 16 * i, n, cols, g, u, y);
+                    if constexpr (EPI == DENSE_GATED_BWD) {
+#pragma unroll
+                        for (int v = 0; v < NV; ++v) {
+                            csg[v] += g[v];
+                            csu[v] += u[v];
+                        }
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    });
+    if constexpr (EPI == DENSE_GATED_BWD)   // a row of column sums for each block of a panel and wave of rows
+        store_colsum<NV>(a, ((int64_t)(i8 / panels) * 8 + x8) * WM + wm, n, csg, csu, r16);
+}
+
+template <int E, int EPI>
+hipError_t launch_narrow(const DenseArgs &a, int kc, int wn, int panels, int64_t blocks, hipStream_t st) {
+    const dim3 grid((unsigned)blocks), block(512);
+    if (kc == 2 && wn == 4) hipLaunchKernelGGL((narrow_kernel<E, 2, 4, EPI>), grid, block, 0, st, a, panels);
+    else if (kc == 2 && wn == 8) hipLaunchKernelGGL((narrow_kernel<E, 2, 8, EPI>), grid, block, 0, st, a, panels);
+    else if (kc == 4 && wn == 4) hipLaunchKernelGGL((narrow_kernel<E, 4, 4, EPI>), grid, block, 0, st, a, panels);
+    else if (kc == 4 && wn == 8) hipLaunchKernelGGL((narrow_kernel<E, 4, 8, EPI>), grid, block, 0, st, a, panels);
+    else if (kc == 8 && wn == 8) hipLaunchKernelGGL((narrow_kernel<E, 8, 8, EPI>), grid, block, 0, st, a, panels);
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace geot

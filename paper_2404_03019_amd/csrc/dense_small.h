@@ -123,28 +123,21 @@ __global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs
         if (in) {
             Columns<4> c;
             load_columns<E, EPI, 4>(a, n, c);
+            float y[4];
+            if constexpr (EPI == DENSE_GATED_BWD) load_wide<E, 4>(a.grad, m * a.ldg + n, a.N - n, y);
             if constexpr (EPI == DENSE_GATED || EPI == DENSE_GATED_BWD)
-                with_act(a.act, [&](auto act) { finish<E, EPI, decltype(act)::value, 4, DUAL>(a, 0, m, n, c, g, u); });
+                with_act(a.act, [&](auto act) { finish<E, EPI, decltype(act)::value, 4, DUAL>(a, 0, m, n, c, g, u, y); });
             else
-                finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, c, g, u);
+                finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, c, g, u, y);
         }
-        if constexpr (EPI == DENSE_GATED_BWD) {
-            if (a.colsum) {   // a row of column sums for each 16 rows
-                float *dst = a.colsum + ((int64_t)tm * FM + i) * 2 * a.N;
+        if constexpr (EPI == DENSE_GATED_BWD) {   // a row of column sums for each 16 rows
+            float sg[4], su[4];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    float sg = in ? g[v] : 0.0f, su = in ? u[v] : 0.0f;
-#pragma unroll
-                    for (int o = 1; o < 16; o <<= 1) {
-                        sg += __shfl_xor(sg, o);
-                        su += __shfl_xor(su, o);
-                    }
-                    if (r16 == 0 && n + v < a.N) {
-                        dst[n + v] = sg;
-                        dst[a.N + n + v] = su;
-                    }
-                }
+            for (int v = 0; v < 4; ++v) {
+                sg[v] = in ? g[v] : 0.0f;
+                su[v] = in ? u[v] : 0.0f;
             }
+            store_colsum<4>(a, (int64_t)tm * FM + i, n, sg, su, r16);
         }
     }
 }

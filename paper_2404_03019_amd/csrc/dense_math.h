@@ -198,10 +198,11 @@ __device__ __forceinline__ void load_columns(const DenseArgs &a, int64_t n, Colu
 
 // Row m, columns n .. n + NV (as many as there are: at least one) of the product. g, u: the sums on entry;
 // DENSE_GATED_BWD takes the incoming gradient in y (0 beyond the last column) and leaves dG, dU in g and u (0
-// there as well).
-template <int E, int EPI, int ACT, int NV, bool DUAL, class Sum>
-__device__ __forceinline__ void finish(const DenseArgs &a, int64_t split, int64_t m, int64_t n, const Columns<NV> &c,
-                                       Sum *g, Sum *u, float *y) {
+// there as well). `at`: where the row's part of the output begins, in elements (m * a.ldo + n). With BIASED
+// the sums of the gated block have started from the biases.
+template <int E, int EPI, int ACT, int NV, bool DUAL, bool BIASED = false, class Sum>
+__device__ __forceinline__ void finish(const DenseArgs &a, int64_t split, int64_t m, int64_t n, int64_t at,
+                                       const Columns<NV> &c, Sum *g, Sum *u, float *y) {
     const int64_t count = a.N - n;
     if constexpr (EPI == DENSE_PART) {
         const int64_t C = DUAL ? 2 * a.N : a.N;
@@ -218,18 +219,19 @@ __device__ __forceinline__ void finish(const DenseArgs &a, int64_t split, int64_
         const float sx = a.sx[m];
 #pragma unroll
         for (int v = 0; v < NV; ++v) y[v] = (float)g[v] * sx * c.p[v] + c.q[v];
-        if (a.out_elem == ELEM_BF16) store_wide<ELEM_BF16, NV>(a.out, m * a.ldo + n, count, y);
-        else if (a.out_elem == ELEM_F16) store_wide<ELEM_F16, NV>(a.out, m * a.ldo + n, count, y);
-        else store_wide<ELEM_F32, NV>(a.out, m * a.ldo + n, count, y);
+        if (a.out_elem == ELEM_BF16) store_wide<ELEM_BF16, NV>(a.out, at, count, y);
+        else if (a.out_elem == ELEM_F16) store_wide<ELEM_F16, NV>(a.out, at, count, y);
+        else store_wide<ELEM_F32, NV>(a.out, at, count, y);
     } else if constexpr (EPI == DENSE_GATED) {
         float d;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) y[v] = activate<E, ACT>(g[v] + c.p[v], &d) * (u[v] + c.q[v]);
+        for (int v = 0; v < NV; ++v)
+            y[v] = BIASED ? activate<E, ACT>(g[v], &d) * u[v] : activate<E, ACT>(g[v] + c.p[v], &d) * (u[v] + c.q[v]);
         if (a.drop.on) {
 #pragma unroll
             for (int v = 0; v < NV; v += 4) drop4(y + v, (uint32_t)((n + v) >> 2), (uint32_t)m, a.drop);
         }
-        store_wide<E, NV>(a.out, m * a.ldo + n, count, y);
+        store_wide<E, NV>(a.out, at, count, y);
     } else {
         if (a.drop.on) {
 #pragma unroll
@@ -238,13 +240,13 @@ __device__ __forceinline__ void finish(const DenseArgs &a, int64_t split, int64_
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             float d;
-            const float h = activate<E, ACT>(g[v] + c.p[v], &d);
+            const float h = activate<E, ACT>(BIASED ? g[v] : g[v] + c.p[v], &d);
             const bool in = v < count;
-            g[v] = in ? y[v] * (u[v] + c.q[v]) * d : 0.0f;
+            g[v] = in ? y[v] * (BIASED ? u[v] : u[v] + c.q[v]) * d : 0.0f;
             u[v] = in ? y[v] * h : 0.0f;
         }
-        store_wide<E, NV>(a.out, m * a.ldo + n, count, g);
-        store_wide<E, NV>(a.out1, m * a.ldo + n, count, u);
+        store_wide<E, NV>(a.out, at, count, g);
+        store_wide<E, NV>(a.out1, at, count, u);
     }
 }
 
@@ -297,7 +299,7 @@ __device__ __forceinline__ void epilogue(const DenseArgs &a, int64_t split, int6
                     }
                     if constexpr (EPI == DENSE_GATED_BWD)
                         load_wide<E, NV>(a.grad, (m + 16 * i) * a.ldg + nj, a.N - nj, y);
-                    finish<E, EPI, ACT, NV, DUAL>(a, split, m + 16 * i, nj, c, g, u, y);
+                    finish<E, EPI, ACT, NV, DUAL>(a, split, m + 16 * i, nj, (m + 16 * i) * a.ldo + nj, c, g, u, y);
                     if constexpr (EPI == DENSE_GATED_BWD) {
 #pragma unroll
                         for (int v = 0; v < NV; ++v) {

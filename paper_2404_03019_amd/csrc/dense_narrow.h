@@ -53,10 +53,17 @@ __global__ void __launch_bounds__(512) narrow_kernel(const DenseArgs a, const in
     }
     Columns<NV> cols;
     load_columns<E, EPI, NV>(a, n, cols);
+    Acc start[FN];   // the sums start from the biases
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) start[j][v] = j < PF ? cols.p[4 * j + v] : cols.q[4 * (j - PF) + v];
     float csg[NV], csu[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) csg[v] = csu[v] = 0.0f;
 
+    const bool whole = n + NV <= a.N;
+    const int64_t row16 = 16 * a.ldo;
     chunk_t stage[C];
     auto fetch = [&](int64_t tile) {
 #pragma unroll
@@ -84,7 +91,7 @@ __global__ void __launch_bounds__(512) narrow_kernel(const DenseArgs a, const in
             land(buf);
             if (tile + stride < tiles) fetch(tile + stride);
             const int64_t m = tile * RT + wm * 16 * FM + r16;
-            const bool whole = n + NV <= a.N;
+            const int64_t at = m * a.ldo + n;
             Wide grad[EPI == DENSE_GATED_BWD ? FM : 1][GW];
             if constexpr (EPI == DENSE_GATED_BWD) {
 #pragma unroll
@@ -106,7 +113,7 @@ __global__ void __launch_bounds__(512) narrow_kernel(const DenseArgs a, const in
                 for (int k = 0; k < KC; ++k) {
                     const chunk_t x = *reinterpret_cast<const chunk_t *>(&lds[buf][row * ROW + (((4 * k + c4) ^ key(row)) << 4)]);
 #pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[j] = mma<E>(w[k][j], x, k ? acc[j] : Acc{0, 0, 0, 0});
+                    for (int j = 0; j < FN; ++j) acc[j] = mma<E>(w[k][j], x, k ? acc[j] : start[j]);
                 }
                 if (n < a.N && m + 16 * i < a.M) {
                     float g[NV], u[NV], y[NV];
@@ -123,7 +130,7 @@ __global__ void __launch_bounds__(512) narrow_kernel(const DenseArgs a, const in
                             load_wide<E, NV>(a.grad, (m + 16 * i) * a.ldg + n, a.N - n, y);
                         }
                     }
-                    finish<E, EPI, decltype(act)::value, NV, true>(a, 0, m + 16 * i, n, cols, g, u, y);
+                    finish<E, EPI, decltype(act)::value, NV, true, true>(a, 0, m + 16 * i, n, at + i * row16, cols, g, u, y);
                     if constexpr (EPI == DENSE_GATED_BWD) {
 #pragma unroll
                         for (int v = 0; v < NV; ++v) {

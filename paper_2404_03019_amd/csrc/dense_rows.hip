@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kRowsBlock) join_kernel(const DenseArgs a) {
         Columns<4> c;
         load_columns<E, EPI, 4>(a, n, c);
         float y[4];
-        finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, c, g, u, y);
+        finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, m * a.ldo + n, c, g, u, y);
     }
 }
 

@@ -126,9 +126,9 @@ __global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs
             float y[4];
             if constexpr (EPI == DENSE_GATED_BWD) load_wide<E, 4>(a.grad, m * a.ldg + n, a.N - n, y);
             if constexpr (EPI == DENSE_GATED || EPI == DENSE_GATED_BWD)
-                with_act(a.act, [&](auto act) { finish<E, EPI, decltype(act)::value, 4, DUAL>(a, 0, m, n, c, g, u, y); });
+                with_act(a.act, [&](auto act) { finish<E, EPI, decltype(act)::value, 4, DUAL>(a, 0, m, n, m * a.ldo + n, c, g, u, y); });
             else
-                finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, c, g, u, y);
+                finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, m * a.ldo + n, c, g, u, y);
         }
         if constexpr (EPI == DENSE_GATED_BWD) {   // a row of column sums for each 16 rows
             float sg[4], su[4];

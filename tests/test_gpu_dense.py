@@ -174,6 +174,27 @@ def test_gated_large_tiles(dtype, M, K, N):
         ref.check(t, *w, f"gradient {i}")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M, K, N, pad", [(17_000, 32, 256, 0), (20_001, 31, 300, 1), (16_385, 64, 20, 0), (9_000, 125, 130, 3),
+                                          (9_001, 128, 40, 0), (8_200, 250, 260, 0), (8_300, 256, 9, 8), (30_000, 1, 70, 0),
+                                          (3_000, 1032, 700, 0), (3_001, 1001, 705, 1)])
+@pytest.mark.parametrize("act, bias, p", [("silu", True, 0.0), ("gelu", False, 0.25), ("relu", True, 0.5)])
+def test_gated_many_rows(dtype, M, K, N, pad, act, bias, p):
+    """Narrow rows (weights kept in registers, panels of columns, ragged tails of each) and wider ones, at odd and
+    even addresses."""
+    g = gen(M + K * 3 + N)
+    x = rand(g, M, K, dtype=dtype, pad=pad)
+    wg, wu = (rand(g, N, K, dtype=dtype, scale=1 / math.sqrt(K), pad=pad) for _ in range(2))
+    bg, bu = (rand(g, N, dtype=dtype) if bias else None for _ in range(2))
+    grad = rand(g, M, N, dtype=dtype, pad=pad)
+    mask = mask_of(M, N, p) if p else None
+    want = ref.gated64(x, wg, wu, bg, bu, act, mask, grad)
+    ref.check(geot.gated_linear(x, wg, wu, bg, bu, act, p, SEED, OFFSET), *want[0], "out")
+    for i, (t, w) in enumerate(zip(geot.gated_linear_backward(grad, x, wg, wu, bg, bu, act, p, SEED, OFFSET), want[1:])):
+        if t is not None:
+            ref.check(t, *w, f"gradient {i}")
+
+
 def test_gated_gradient_against_differences():
     """fp32 gradients against central differences of the block in 64 bits (whose error is of the order of h^2)."""
     M, K, N, h = 5, 9, 6, 1e-4

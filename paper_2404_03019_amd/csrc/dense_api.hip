@@ -153,7 +153,8 @@ DensePlan plan_dense(int elem, int epi, int mode, int64_t M, int64_t N, int64_t 
     const int64_t tiles = std::max<int64_t>(1, p.tiles_m * p.tiles_n);
     p.steps_per = (int64_t)1 << 40;   // all of them
     if (p.tile == DENSE_TILE_128 && epi != DENSE_GATED_BWD && tiles < kDenseCUs && steps > 1) {
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2 * kDenseCUs / tiles, steps / 2));
+        // short parts where a few tiles hold all (weight gradients); else a part has to pay for the join
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2 * kDenseCUs / tiles, steps / (tiles < 16 ? 2 : 4)));
         p.steps_per = up(up(steps, want), 2) * 2;   // even: the kernel takes steps in pairs
         p.splits = up(steps, p.steps_per);
     }

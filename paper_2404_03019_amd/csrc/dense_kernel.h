@@ -504,7 +504,7 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
 template <int E, int EPI, bool DUAL, int MODE>
 hipError_t launch_tile(int tile, bool direct, const DenseArgs &a, int64_t blocks, hipStream_t st) {
     const dim3 grid((unsigned)blocks);
-    if constexpr (E != ELEM_F32) {
+    if constexpr (E != ELEM_F32 && EPI != DENSE_PART) {
         if (tile == DENSE_TILE_256) {
             hipLaunchKernelGGL((dense_kernel<E, 256, 256, 2, 2, EPI, DUAL, MODE, true>), grid, dim3(256), 0, st, a);
             return hipGetLastError();

@@ -181,7 +181,12 @@ __global__ void __launch_bounds__(kRowsBlock) join_kernel(const DenseArgs a) {
         Columns<4> c;
         load_columns<E, EPI, 4>(a, n, c);
         float y[4];
-        finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, m * a.ldo + n, c, g, u, y);
+        if constexpr (EPI == DENSE_GATED)
+            with_act(a.act, [&](auto act) {
+                finish<E, EPI, decltype(act)::value, 4, DUAL>(a, 0, m, n, m * a.ldo + n, c, g, u, y);
+            });
+        else
+            finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, m * a.ldo + n, c, g, u, y);
     }
 }
 
@@ -263,6 +268,7 @@ hipError_t join_of(const DenseArgs &a, hipStream_t st) {
 
 template <int E>
 hipError_t join_float(int epi, const DenseArgs &a, hipStream_t st) {
+    if (epi == DENSE_GATED) return join_of<E, DENSE_GATED, true>(a, st);
     if (epi == DENSE_PLAIN) return join_of<E, DENSE_PLAIN, false>(a, st);
     return hipErrorInvalidValue;
 }

@@ -157,7 +157,7 @@ def _dev(t: torch.Tensor, name: str, dtype, ndim):
 
 
 def _shape(t: torch.Tensor | None, name: str, shape: tuple):
-    if t is not None and tuple(t.shape) != tuple(shape):
+    if t is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
@@ -204,6 +204,7 @@ class _OnDevice:
 
 # storage types of src / x and index types accepted by the typed entry points
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_FLOATS = tuple(DTYPES)
 INDEX_TYPES = {torch.int64: 0, torch.int32: 1}
 
 
@@ -620,7 +621,7 @@ def _rows(t: torch.Tensor, name: str, dtype) -> int:
     columns); its row stride in elements."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+    if t.dtype is not dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
         raise TypeError(f"{name} must be {dtype}")
     if t.dim() != 2:
         raise ValueError(f"{name} must have 2 dimensions")
@@ -638,6 +639,17 @@ def _rows(t: torch.Tensor, name: str, dtype) -> int:
 
 def _ptr(t: torch.Tensor | None):
     return t.data_ptr() if t is not None else None
+
+
+def _launch(call, device: int, *args):
+    """call(*args, stream) on that device's current stream, with the device current."""
+    if torch._C._cuda_getDevice() == device:
+        st = call(*args, torch._C._cuda_getCurrentRawStream(device))
+    else:
+        with torch.cuda.device(device):
+            st = call(*args, torch._C._cuda_getCurrentRawStream(device))
+    if st:
+        _raise(st)
 
 
 def _mask_args(p, seed, offset):
@@ -659,7 +671,7 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual: tor
         o2 = out[None] if out is not None and out.dim() == 1 else out
         y = dropout(x[None], p, seed, offset, r2, o2)
         return out if out is not None else y[0]
-    ld = _rows(x, "x", tuple(DTYPES))
+    ld = _rows(x, "x", _FLOATS)
     p, seed, offset = _mask_args(p, seed, offset)
     R, F = x.shape
     ldr = ldo = F
@@ -672,17 +684,15 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual: tor
     _on_gpu(x=x, residual=residual, out=out)
     if out is None:
         out = torch.empty((R, F), dtype=x.dtype, device=x.device)
-    with _OnDevice(x.device):
-        st = lib().geot_dropout(x.data_ptr(), DTYPES[x.dtype], R, F, ld, _ptr(residual), ldr, p, seed, offset,
-                                out.data_ptr(), ldo, _stream(x.device))
-    _raise(st)
+    _launch(lib().geot_dropout, x.get_device(), x.data_ptr(), DTYPES[x.dtype], R, F, ld, _ptr(residual), ldr, p, seed,
+            offset, out.data_ptr(), ldo)
     return out
 
 
 def _gated_args(x, w_gate, w_up, b_gate, b_up, act, p, seed, offset):
     """The arguments that the gated block's forward and gradients share, checked: (x's row stride, the
     weights' row stride, (p, seed, offset))."""
-    ld = _rows(x, "x", tuple(DTYPES))
+    ld = _rows(x, "x", _FLOATS)
     ldw = _rows(w_gate, "w_gate", x.dtype)
     ldu = _rows(w_up, "w_up", x.dtype)
     N, K = w_gate.shape
@@ -716,11 +726,8 @@ def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_ga
     _on_gpu(x=x, w_gate=w_gate, w_up=w_up, b_gate=b_gate, b_up=b_up, out=out)
     if out is None:
         out = torch.empty((M, N), dtype=x.dtype, device=x.device)
-    with _OnDevice(x.device):
-        st = lib().geot_gated_linear(x.data_ptr(), DTYPES[x.dtype], M, K, ld, w_gate.data_ptr(), w_up.data_ptr(), N,
-                                     ldw, _ptr(b_gate), _ptr(b_up), ACTIVATIONS[act], p, seed, offset, out.data_ptr(),
-                                     ldo, _stream(x.device))
-    _raise(st)
+    _launch(lib().geot_gated_linear, x.get_device(), x.data_ptr(), DTYPES[x.dtype], M, K, ld, w_gate.data_ptr(),
+            w_up.data_ptr(), N, ldw, _ptr(b_gate), _ptr(b_up), ACTIVATIONS[act], p, seed, offset, out.data_ptr(), ldo)
     return out
 
 
@@ -741,12 +748,9 @@ def gated_linear_backward(grad_out: torch.Tensor, x: torch.Tensor, w_gate: torch
 
     gx, gwg, gwu = empty(need_x, M, K), empty(need_w, N, K), empty(need_w, N, K)
     gbg, gbu = empty(need_b and b_gate is not None, N), empty(need_b and b_up is not None, N)
-    with _OnDevice(x.device):
-        st = lib().geot_gated_linear_backward(grad_out.data_ptr(), ldg, x.data_ptr(), DTYPES[x.dtype], M, K, ld,
-                                              w_gate.data_ptr(), w_up.data_ptr(), N, ldw, _ptr(b_gate), _ptr(b_up),
-                                              ACTIVATIONS[act], p, seed, offset, _ptr(gx), _ptr(gwg), _ptr(gwu),
-                                              _ptr(gbg), _ptr(gbu), _stream(x.device))
-    _raise(st)
+    _launch(lib().geot_gated_linear_backward, x.get_device(), grad_out.data_ptr(), ldg, x.data_ptr(), DTYPES[x.dtype],
+            M, K, ld, w_gate.data_ptr(), w_up.data_ptr(), N, ldw, _ptr(b_gate), _ptr(b_up), ACTIVATIONS[act], p, seed,
+            offset, _ptr(gx), _ptr(gwg), _ptr(gwu), _ptr(gbg), _ptr(gbu))
     return gx, gwg, gwu, gbg, gbu
 
 
@@ -755,15 +759,13 @@ def quantize_rows(x: torch.Tensor):
 
     x [rows, F] fp32, bf16 or fp16; q int8 [rows, F], scale fp32 [rows]. A row that holds NaN or an infinity
     gets scale NaN."""
-    ld = _rows(x, "x", tuple(DTYPES))
+    ld = _rows(x, "x", _FLOATS)
     _on_gpu(x=x)
     R, F = x.shape
     q = torch.empty((R, F), dtype=torch.int8, device=x.device)
     scale = torch.empty(R, dtype=torch.float32, device=x.device)
-    with _OnDevice(x.device):
-        st = lib().geot_quantize_rows(x.data_ptr(), DTYPES[x.dtype], R, F, ld, q.data_ptr(), max(F, 1), scale.data_ptr(),
-                                      _stream(x.device))
-    _raise(st)
+    _launch(lib().geot_quantize_rows, x.get_device(), x.data_ptr(), DTYPES[x.dtype], R, F, ld, q.data_ptr(), max(F, 1),
+            scale.data_ptr())
     return q, scale
 
 
@@ -778,10 +780,10 @@ def linear_int8(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_sca
     M, K = xq.shape
     N = wq.shape[0]
     _shape(wq, "wq", (N, K))
-    for name, t, n in (("x_scale", x_scale, M), ("w_scale", w_scale, N), ("bias", bias, N)):
-        if t is not None or name != "bias":
-            _dev(t, name, torch.float32, 1)
-            _shape(t, name, (n,))
+    _shape(_dev(x_scale, "x_scale", torch.float32, 1), "x_scale", (M,))
+    _shape(_dev(w_scale, "w_scale", torch.float32, 1), "w_scale", (N,))
+    if bias is not None:
+        _shape(_dev(bias, "bias", torch.float32, 1), "bias", (N,))
     if dtype not in DTYPES:
         raise TypeError(f"dtype must be one of {tuple(DTYPES)}")
     ldo = N
@@ -791,10 +793,8 @@ def linear_int8(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_sca
     _on_gpu(xq=xq, x_scale=x_scale, wq=wq, w_scale=w_scale, bias=bias, out=out)
     if out is None:
         out = torch.empty((M, N), dtype=dtype, device=xq.device)
-    with _OnDevice(xq.device):
-        st = lib().geot_linear_int8(xq.data_ptr(), x_scale.data_ptr(), M, K, ldx, wq.data_ptr(), w_scale.data_ptr(), N,
-                                    ldw, _ptr(bias), out.data_ptr(), DTYPES[dtype], ldo, _stream(xq.device))
-    _raise(st)
+    _launch(lib().geot_linear_int8, xq.get_device(), xq.data_ptr(), x_scale.data_ptr(), M, K, ldx, wq.data_ptr(),
+            w_scale.data_ptr(), N, ldw, _ptr(bias), out.data_ptr(), DTYPES[dtype], ldo)
     return out
 
 

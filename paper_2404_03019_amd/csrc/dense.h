@@ -33,8 +33,14 @@ enum DenseMode : int {
 };
 
 // DENSE_TILE_SMALL: blocks of 16 fm rows and 16 fn weight rows, whose waves share K. DENSE_TILE_NARROW: rows of
-// up to 64 fm bytes, fn waves over the columns; a block goes on to further rows.
-enum DenseTile : int { DENSE_TILE_128 = 0, DENSE_TILE_256 = 1, DENSE_TILE_SMALL = 2, DENSE_TILE_NARROW = 3 };
+// up to 64 fm bytes, fn waves over the columns; a block goes on to further rows. DENSE_TILE_32: 128 x 32.
+enum DenseTile : int {
+    DENSE_TILE_128 = 0,
+    DENSE_TILE_256 = 1,
+    DENSE_TILE_SMALL = 2,
+    DENSE_TILE_NARROW = 3,
+    DENSE_TILE_32 = 4,
+};
 
 // C[m, n] = sum_k A[m, k] B[n, k]. With DENSE_NT and b1 there are two column operands: g comes from b0 and u
 // from b1, N columns each. With DENSE_NN and b1 K comes twice: A's second K columns start seg_a bytes

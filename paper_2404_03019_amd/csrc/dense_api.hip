@@ -147,12 +147,13 @@ DensePlan plan_dense(int elem, int epi, int mode, int64_t M, int64_t N, int64_t 
     if (direct && elem != ELEM_F32 && t_big >= kDenseCUs &&
         up(t_big, kDenseCUs) * (70 + 16 * steps) < up(t_small, 2 * kDenseCUs) * (30 + 10 * steps))
         p.tile = DENSE_TILE_256;
+    if (mode != DENSE_NT && N <= 64) p.tile = DENSE_TILE_32;   // gradients of narrow features
     const int64_t tile = p.tile == DENSE_TILE_256 ? 256 : 128;
     p.tiles_m = up(M, tile);
-    p.tiles_n = up(N, dual ? tile / 2 : tile);
+    p.tiles_n = up(N, p.tile == DENSE_TILE_32 ? 32 : dual ? tile / 2 : tile);
     const int64_t tiles = std::max<int64_t>(1, p.tiles_m * p.tiles_n);
     p.steps_per = (int64_t)1 << 40;   // all of them
-    if (p.tile == DENSE_TILE_128 && epi != DENSE_GATED_BWD && tiles < kDenseCUs && steps > 1) {
+    if (p.tile != DENSE_TILE_256 && epi != DENSE_GATED_BWD && tiles < kDenseCUs && steps > 1) {
         // short parts where a few tiles hold all (weight gradients); else a part has to pay for the join
         const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2 * kDenseCUs / tiles, steps / (tiles < 16 ? 2 : 4)));
         p.steps_per = up(up(steps, want), 2) * 2;   // even: the kernel takes steps in pairs

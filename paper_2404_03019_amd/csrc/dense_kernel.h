@@ -164,9 +164,9 @@ struct Tile {
             else return row & 7;
         } else if constexpr (ES == 2) {
             // a transposing read takes four rows from each of several runs of eight in one cycle
-            return ((row & 3) << 1) | ((((row >> 3) ^ (row >> 4)) & 1) << 3);
+            return (((row & 3) << 1) | ((((row >> 3) ^ (row >> 4)) & 1) << 3)) & (CPR - 1);
         } else {
-            return ((row >> 2) & 3) << 2;
+            return (((row >> 2) & 3) << 2) & (CPR - 1);
         }
     }
     // chunk i: its row of LDS, and the chunk of that row in memory that it holds
@@ -230,6 +230,7 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
     typedef Tile<E, BM, KA, 0> TA;
     typedef Tile<E, BN, KB, KB ? 0 : 4 * PF> TB;
     typedef typename AccOf<E>::type Acc;
+    static_assert(BN * 8 % T == 0 && BM * 8 % T == 0, "whole chunks a thread");
     static_assert(!DUAL || MODE == DENSE_NT, "two column operands have k along their rows");
     __shared__ __align__(16) char lds0[(BM + BN) * kStepBytes];
     __shared__ __align__(16) char lds1[(BM + BN) * kStepBytes];
@@ -507,6 +508,15 @@ hipError_t launch_tile(int tile, bool direct, const DenseArgs &a, int64_t blocks
     if constexpr (E != ELEM_F32 && EPI != DENSE_PART) {
         if (tile == DENSE_TILE_256) {
             hipLaunchKernelGGL((dense_kernel<E, 256, 256, 2, 2, EPI, DUAL, MODE, true>), grid, dim3(256), 0, st, a);
+            return hipGetLastError();
+        }
+    }
+    if constexpr (MODE != DENSE_NT) {
+        if (tile == DENSE_TILE_32) {
+            if (direct)
+                hipLaunchKernelGGL((dense_kernel<E, 128, 32, 4, 1, EPI, DUAL, MODE, true>), grid, dim3(256), 0, st, a);
+            else
+                hipLaunchKernelGGL((dense_kernel<E, 128, 32, 4, 1, EPI, DUAL, MODE, false>), grid, dim3(256), 0, st, a);
             return hipGetLastError();
         }
     }

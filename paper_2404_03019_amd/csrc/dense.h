@@ -99,6 +99,11 @@ hipError_t launch_colsum(int elem, const float *colsum, int64_t rows, int64_t N,
                          hipStream_t st);
 constexpr int64_t kColsumMid = 64;  // rows of `mid`, [kColsumMid x 2N]
 
+// rows of `bytes` bytes, src_ld apart, to dst_ld apart (a multiple of 16, at least `bytes`; dst on 16 bytes); what
+// a row of dst has beyond is 0 to the next multiple of 16
+hipError_t launch_align_rows(const void *src, int64_t src_ld, int64_t rows, int64_t bytes, void *dst, int64_t dst_ld,
+                             hipStream_t st);
+
 hipError_t launch_dropout(int elem, const void *x, int64_t ldx, const void *res, int64_t ldr, int64_t rows, int64_t F,
                           const Drop &d, void *out, int64_t ldo, hipStream_t st);
 hipError_t launch_quantize_rows(int elem, const void *x, int64_t ldx, int64_t rows, int64_t F, int8_t *q, int64_t ldq,

@@ -106,10 +106,14 @@ geot_status_t make_drop(double p, uint64_t seed, uint64_t offset, int64_t rows, 
 
 // Whether every whole step of an operand can be loaded straight into LDS: 16-byte chunks at 16-byte
 // addresses, at offsets of 32 bits from the tile's first element; with a row per k (`cols` of them) chunks
-// wholly inside or outside the columns.
+// wholly inside or outside the columns. 256 rows stay within 32 bits up to this stride in bytes.
+constexpr int64_t kDirectStride = (int64_t)1 << 23;
 static bool direct_ok(const void *p, int64_t ld, int64_t es, int64_t cols = 0) {
-    return ((uintptr_t)p & 15) == 0 && ld * es % 16 == 0 && ld * es < ((int64_t)1 << 23) && cols * es % 16 == 0;
+    return ((uintptr_t)p & 15) == 0 && ld * es % 16 == 0 && ld * es < kDirectStride && cols * es % 16 == 0;
 }
+
+// Few rows, or tiles for less than half the chip (C columns in all).
+static bool few_tiles(int64_t M, int64_t C) { return M <= 64 || up(M, 128) * up(C, 128) < kDenseCUs / 2; }
 
 DensePlan plan_dense(int elem, int epi, int mode, int64_t M, int64_t N, int64_t K, bool dual, int segments, bool direct) {
     DensePlan p{DENSE_TILE_128, 0, 0, 0, direct, 1, 0, 0, 0, 0, 0};
@@ -120,8 +124,8 @@ DensePlan plan_dense(int elem, int epi, int mode, int64_t M, int64_t N, int64_t 
     // 66 / 55. fp32, whose multiplications take eight times as long, gains nothing from the larger tile
     // (16,384 rows, 1,024 -> 2,048 1,059 / 1,056 us).
     const int64_t t_big = up(M, 256) * up(C, 256), t_small = up(M, 128) * up(C, 128);
-    if (mode == DENSE_NT && (M <= 64 || t_small < kDenseCUs / 2)) {
-        // Few rows, or tiles for less than half the chip: blocks of up to 64 rows whose waves share K. As many
+    if (mode == DENSE_NT && few_tiles(M, C)) {
+        // Blocks of up to 64 rows whose waves share K. As many
         // weight rows a block as still give every CU a block.
         p.tile = DENSE_TILE_SMALL;
         p.fm = M <= 16 ? 1 : M <= 32 ? 2 : 4;
@@ -204,13 +208,78 @@ geot_status_t check_gated(const Gated &q, geot_activation_t act) {
     return GEOT_SUCCESS;
 }
 
-
-
 bool gated_direct(const Gated &q) {
     return direct_ok(q.x.p, q.x.ld, q.x.es) && direct_ok(q.wg.p, q.wg.ld, q.x.es) && direct_ok(q.wu.p, q.wu.ld, q.x.es);
 }
 
-geot_status_t gated_forward(const Gated &q, geot_activation_t act, const Drop &drop, const Mat &out, hipStream_t st) {
+// Temporary memory of a call, laid out before it is taken.
+struct Layout {
+    size_t bytes = 0;
+    size_t take(size_t n) {
+        const size_t at = bytes;
+        bytes = (bytes + n + 255) & ~(size_t)255;
+        return at;
+    }
+};
+
+// Operands at other than 16-byte addresses and strides go through registers, where large products lose up to
+// half their rate. Whether copies of them in aligned rows pay for themselves, measured without / with, bf16
+// (x and both weights copied):
+//   gradients, three products of the same operands: from 192 columns and 65 features. 20,000 rows, 3,533 -> 192
+//     417 / 357 us, -> 1,536 2,642 / 1,762; 515 -> 192 98 / 94; 100 -> 256 71 / 68; 237,472 rows, 100 -> 1,024
+//     1,283 / 895; but -> 96 182 / 195, and 50 -> 256 242 / 253.
+//   forward, one product: only long rows and many of them. 20,000 rows, 3,533 -> 768 357 / 306, -> 1,536
+//     689 / 534 (8-bit 116 / 114, 222 / 180), but -> 384 183 / 214; 515 -> 1,536 146 / 148; 3,000 rows, 1,217 ->
+//     1,536 65 / 71.
+// fp32 is bound by its multiplications either way.
+bool worth_aligning(int elem, int64_t M, int64_t N, int64_t K, bool dual, bool gradients) {
+    const int64_t kbytes = K * elem_bytes(elem);
+    if (elem == ELEM_F32 || few_tiles(M, dual ? 2 * N : N) || kbytes >= kDirectStride - 16) return false;
+    if (gradients) return N >= 192 && K > 64;
+    return N >= 768 && kbytes >= 2048 && (double)M * (double)N * (double)K >= 2e10;
+}
+
+// Copies of the operands that are not aligned, in rows of Kp elements.
+struct Aligned {
+    bool x = false, w = false;
+    int64_t Kp = 0;
+    size_t o_x = 0, o_wg = 0, o_wu = 0;
+    void plan(const Mat &mx, const Mat &mg, const Mat *mu, int elem, bool gradients, Layout *lay) {
+        const int64_t es = mx.es;
+        if (!worth_aligning(elem, mx.rows, mg.rows, mx.cols, mu != nullptr, gradients)) return;
+        x = !direct_ok(mx.p, mx.ld, es);
+        w = !direct_ok(mg.p, mg.ld, es) || (mu && !direct_ok(mu->p, mu->ld, es));
+        Kp = up(mx.cols, 16 / es) * (16 / es);
+        if (x) o_x = lay->take((size_t)(mx.rows * Kp * es));
+        if (w) o_wg = lay->take((size_t)(mg.rows * Kp * es));
+        if (w && mu) o_wu = lay->take((size_t)(mu->rows * Kp * es));
+    }
+    static geot_status_t one(Mat *m, char *to, int64_t Kp, hipStream_t st) {
+        DENSE_HIP(launch_align_rows(m->p, m->ld * m->es, m->rows, m->cols * m->es, to, Kp * m->es, st), "launch aligned copy");
+        m->p = to;
+        m->ld = Kp;
+        return GEOT_SUCCESS;
+    }
+    // makes the copies, and the arguments name them
+    geot_status_t make(char *base, Mat *mx, Mat *mg, Mat *mu, hipStream_t st) const {
+        if (x) DENSE_TRY(one(mx, base + o_x, Kp, st));
+        if (w) DENSE_TRY(one(mg, base + o_wg, Kp, st));
+        if (w && mu) DENSE_TRY(one(mu, base + o_wu, Kp, st));
+        return GEOT_SUCCESS;
+    }
+};
+
+geot_status_t gated_forward(Gated q, geot_activation_t act, const Drop &drop, const Mat &out, hipStream_t st) {
+    Layout lay;
+    Aligned al;
+    al.plan(q.x, q.wg, &q.wu, q.elem, false, &lay);
+    const bool direct = gated_direct(q) || al.x || al.w;
+    const DensePlan plan = plan_dense(q.elem, DENSE_GATED, DENSE_NT, q.M, q.N, q.K, true, 1, direct);
+    const size_t o_part = lay.take(plan.part_bytes);
+    CallMemory mem(st);
+    char *base = nullptr;
+    DENSE_TRY(mem.get(lay.bytes, &base));
+    DENSE_TRY(al.make(base, &q.x, &q.wg, &q.wu, st));
     DenseArgs a;
     a.a = q.x.p;
     a.lda = q.x.ld;
@@ -226,11 +295,7 @@ geot_status_t gated_forward(const Gated &q, geot_activation_t act, const Drop &d
     a.drop = drop;
     a.out = const_cast<void *>(out.p);
     a.ldo = out.ld;
-    const DensePlan plan = plan_dense(q.elem, DENSE_GATED, DENSE_NT, q.M, q.N, q.K, true, 1, gated_direct(q));
-    CallMemory mem(st);
-    char *part = nullptr;
-    DENSE_TRY(mem.get(plan.part_bytes, &part));
-    a.part = part;
+    a.part = base + o_part;
     DENSE_HIP(launch_dense(q.elem, DENSE_GATED, DENSE_NT, a, plan, st), "launch gated product");
     return GEOT_SUCCESS;
 }
@@ -296,7 +361,7 @@ geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stri
         DENSE_TRY(check_type((int)type));
         const int elem = (int)type;
         const int64_t es = elem_bytes(elem), M = rows, K = in_features, N = out_features;
-        const Gated q{{"x", x, M, K, x_stride, es}, {"w_gate", w_gate, N, K, w_stride, es}, {"w_up", w_up, N, K, w_stride, es},
+        Gated q{{"x", x, M, K, x_stride, es}, {"w_gate", w_gate, N, K, w_stride, es}, {"w_up", w_up, N, K, w_stride, es},
                       b_gate, b_up, M, K, N, elem};
         DENSE_TRY(check_gated(q, act));
         const Mat mg{"grad_out", grad_out, M, N, grad_stride, es};
@@ -324,31 +389,31 @@ geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stri
         // separate projections would have. Each starts on 16 bytes in every row.
         const int64_t lane = 16 / es, Np = up(N, lane) * lane;
         const int64_t ld2 = 2 * Np + (2 * Np * es % 2048 == 0 ? 128 / es : 0);   // rows not all on one memory channel
-        const DensePlan p0 = plan_dense(elem, DENSE_GATED_BWD, DENSE_NT, M, N, K, true, 1, gated_direct(q));
-        const DensePlan px = plan_dense(elem, DENSE_PLAIN, DENSE_NN, M, K, N, false, 2,
-                                        direct_ok(w_gate, w_stride, es, K) && direct_ok(w_up, w_stride, es, K) && ld2 * es < ((int64_t)1 << 23));
-        const DensePlan pw = plan_dense(elem, DENSE_PLAIN, DENSE_TN, 2 * Np, K, M, false, 1,
-                                        direct_ok(x, x_stride, es, K) && ld2 * es < ((int64_t)1 << 23));
-        size_t at = 0;
-        auto take = [&](size_t b) {
-            const size_t o = at;
-            at = (at + b + 255) & ~(size_t)255;
-            return o;
-        };
-        const size_t o_d = take((size_t)(M * ld2 * es));
-        const size_t o_cs = need_b ? take((size_t)(p0.colsum_rows * 2 * N) * 4) : 0;
-        const size_t o_mid = need_b ? take((size_t)(kColsumMid * 2 * N) * 4) : 0;
-        const size_t o_part = take(std::max(need_x ? px.part_bytes : 0, need_w ? pw.part_bytes : 0));
+        Layout lay;
+        Aligned al;
+        al.plan(q.x, q.wg, &q.wu, elem, true, &lay);
+        // where the features' rows are copies every 16-byte chunk of them may be read
+        const int64_t x_cols = al.x ? al.Kp : K, w_cols = al.w ? al.Kp : K;
+        const bool x_ok = al.x || direct_ok(x, x_stride, es), rows_ok = ld2 * es < kDirectStride;
+        const bool w_ok = al.w || (direct_ok(w_gate, w_stride, es) && direct_ok(w_up, w_stride, es));
+        const DensePlan p0 = plan_dense(elem, DENSE_GATED_BWD, DENSE_NT, M, N, K, true, 1, x_ok && w_ok);
+        const DensePlan px = plan_dense(elem, DENSE_PLAIN, DENSE_NN, M, K, N, false, 2, w_ok && w_cols % lane == 0 && rows_ok);
+        const DensePlan pw = plan_dense(elem, DENSE_PLAIN, DENSE_TN, 2 * Np, K, M, false, 1, x_ok && x_cols % lane == 0 && rows_ok);
+        const size_t o_d = lay.take((size_t)(M * ld2 * es));
+        const size_t o_cs = need_b ? lay.take((size_t)(p0.colsum_rows * 2 * N) * 4) : 0;
+        const size_t o_mid = need_b ? lay.take((size_t)(kColsumMid * 2 * N) * 4) : 0;
+        const size_t o_part = lay.take(std::max(need_x ? px.part_bytes : 0, need_w ? pw.part_bytes : 0));
         CallMemory mem(st);
         char *base = nullptr;
-        DENSE_TRY(mem.get(at, &base));
+        DENSE_TRY(mem.get(lay.bytes, &base));
+        DENSE_TRY(al.make(base, &q.x, &q.wg, &q.wu, st));
         if (M > 0 && N > 0) {
             DenseArgs a;
-            a.a = x;
-            a.lda = x_stride;
-            a.b0 = w_gate;
-            a.b1 = w_up;
-            a.ldb = w_stride;
+            a.a = q.x.p;
+            a.lda = q.x.ld;
+            a.b0 = q.wg.p;
+            a.b1 = q.wu.p;
+            a.ldb = q.wg.ld;
             a.M = M;
             a.N = N;
             a.K = K;
@@ -373,9 +438,9 @@ geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stri
             a.a = base + o_d;
             a.lda = ld2;
             a.seg_a = Np * es;
-            a.b0 = w_gate;
-            a.b1 = w_up;
-            a.ldb = w_stride;
+            a.b0 = q.wg.p;
+            a.b1 = q.wu.p;
+            a.ldb = q.wg.ld;
             a.M = M;
             a.N = K;
             a.K = N;
@@ -388,8 +453,8 @@ geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stri
             DenseArgs a;
             a.a = base + o_d;
             a.lda = ld2;
-            a.b0 = x;
-            a.ldb = x_stride;
+            a.b0 = q.x.p;
+            a.ldb = q.x.ld;
             a.M = 2 * Np;
             a.N = K;
             a.K = M;
@@ -430,7 +495,7 @@ geot_status_t geot_linear_int8(const int8_t *xq, const float *x_scale, int64_t r
     return guarded([&]() -> geot_status_t {
         DENSE_TRY(check_type((int)out_type));
         const int64_t M = rows, K = in_features, N = out_features;
-        const Mat mx{"xq", xq, M, K, x_stride, 1}, mw{"wq", wq, N, K, w_stride, 1};
+        Mat mx{"xq", xq, M, K, x_stride, 1}, mw{"wq", wq, N, K, w_stride, 1};
         const Mat mo{"out", out, M, N, out_stride, elem_bytes((int)out_type)};
         const Mat sx{"x_scale", x_scale, 1, M, M, 4}, sw{"w_scale", w_scale, 1, N, N, 4}, mb{"bias", bias, 1, N, N, 4};
         for (const Mat &m : {mx, mw, mo, sx, sw}) DENSE_TRY(check_mat(m));
@@ -440,11 +505,21 @@ geot_status_t geot_linear_int8(const int8_t *xq, const float *x_scale, int64_t r
         for (const Mat &m : {mx, mw, sx, sw, mb}) DENSE_TRY(check_apart(mo, m));
         if (M == 0 || N == 0) return GEOT_SUCCESS;
         hipStream_t st = (hipStream_t)stream;
+        Layout lay;
+        Aligned al;
+        al.plan(mx, mw, nullptr, ELEM_I8, false, &lay);
+        const bool direct = (al.x || direct_ok(xq, x_stride, 1)) && (al.w || direct_ok(wq, w_stride, 1));
+        const DensePlan plan = plan_dense(ELEM_I8, DENSE_I8, DENSE_NT, M, N, K, false, 1, direct);
+        const size_t o_part = lay.take(plan.part_bytes);
+        CallMemory mem(st);
+        char *base = nullptr;
+        DENSE_TRY(mem.get(lay.bytes, &base));
+        DENSE_TRY(al.make(base, &mx, &mw, nullptr, st));
         DenseArgs a;
-        a.a = xq;
-        a.lda = x_stride;
-        a.b0 = wq;
-        a.ldb = w_stride;
+        a.a = mx.p;
+        a.lda = mx.ld;
+        a.b0 = mw.p;
+        a.ldb = mw.ld;
         a.M = M;
         a.N = N;
         a.K = K;
@@ -454,11 +529,7 @@ geot_status_t geot_linear_int8(const int8_t *xq, const float *x_scale, int64_t r
         a.out = out;
         a.out_elem = (int)out_type;
         a.ldo = out_stride;
-        const DensePlan plan = plan_dense(ELEM_I8, DENSE_I8, DENSE_NT, M, N, K, false, 1, direct_ok(xq, x_stride, 1) && direct_ok(wq, w_stride, 1));
-        CallMemory mem(st);
-        char *part = nullptr;
-        DENSE_TRY(mem.get(plan.part_bytes, &part));
-        a.part = part;
+        a.part = base + o_part;
         DENSE_HIP(launch_dense(ELEM_I8, DENSE_I8, DENSE_NT, a, plan, st), "launch 8-bit product");
         return GEOT_SUCCESS;
     });

@@ -3,7 +3,7 @@
 // C[m, n] = sum_k A[m, k] B[n, k]: rows m are graph nodes (tokens) and columns n output channels; in the
 // gradients m or n is a feature and k a channel or a node. A block takes a BM x BN tile and walks K in
 // steps of 128 bytes (64 16-bit, 32 fp32 or 128 8-bit elements), so one layout serves every type. An operand
-// lies in memory either with k along its rows () or with a row per k:
+// lies in memory either with k along its rows or with a row per k:
 //   rows of k:  a tile of R rows is R x 128 bytes in LDS. A lane's operand of a 16 x 16 matrix instruction is
 //               one 16-byte chunk of its row (k in the order of the chunks, the same for both operands, so
 //               the order inside K does not matter).

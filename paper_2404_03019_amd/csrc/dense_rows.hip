@@ -219,6 +219,29 @@ __global__ void __launch_bounds__(kRowsBlock) colsum_kernel(const float *sums, i
     if (out) store_wide<E, 1>(out, c < N ? c : c - N, 1, &s);
 }
 
+// 16 bytes a thread; the last of a row that is no multiple of 16 by bytes
+__global__ void __launch_bounds__(kRowsBlock) align_rows_kernel(const char *src, int64_t src_ld, int64_t rows, int64_t bytes,
+                                                                const RowGrid grid, char *dst, int64_t dst_ld) {
+    const int64_t rb = blockIdx.x / grid.chunks, chunk = blockIdx.x - rb * grid.chunks;
+    const uint32_t row = threadIdx.x / (uint32_t)grid.width, lane = threadIdx.x - row * grid.width;
+    const int64_t at = (chunk * grid.width + lane) * 16, left = bytes - at;
+    if (row >= (uint32_t)grid.rows || left <= 0) return;
+    typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(1)));
+    typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+    for (int64_t r = rb * grid.rows + row; r < rows; r += grid.row_blocks * grid.rows) {
+        const char *p = src + r * src_ld + at;
+        word4 v = {0, 0, 0, 0};
+        if (left >= 16) {
+            v = *reinterpret_cast<const any4 *>(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (i < left) v[i / 4] |= (uint32_t)(uint8_t)p[i] << (i % 4 * 8);
+        }
+        *reinterpret_cast<word4 *>(dst + r * dst_ld + at) = v;
+    }
+}
+
 template <int E>
 hipError_t dropout_of(const void *x, int64_t ldx, const void *res, int64_t ldr, int64_t rows, int64_t F, const Drop &d,
                       void *out, int64_t ldo, hipStream_t st) {
@@ -281,6 +304,16 @@ hipError_t colsum_of(const float *sums, int64_t rows, int64_t N, void *out0, voi
 }
 
 }  // namespace
+
+hipError_t launch_align_rows(const void *src, int64_t src_ld, int64_t rows, int64_t bytes, void *dst, int64_t dst_ld,
+                             hipStream_t st) {
+    if (rows <= 0 || bytes <= 0) return hipSuccess;
+    const RowGrid g = row_grid(rows, (bytes + 1) / 2, 16384);   // groups of 8 16-bit columns
+    if (g.chunks * g.row_blocks > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(align_rows_kernel, dim3((unsigned)(g.chunks * g.row_blocks)), dim3(kRowsBlock), 0, st,
+                       (const char *)src, src_ld, rows, bytes, g, (char *)dst, dst_ld);
+    return hipGetLastError();
+}
 
 hipError_t launch_dropout(int elem, const void *x, int64_t ldx, const void *res, int64_t ldr, int64_t rows, int64_t F,
                           const Drop &d, void *out, int64_t ldo, hipStream_t st) {

@@ -178,7 +178,7 @@ def test_gated_large_tiles(dtype, M, K, N):
 @pytest.mark.parametrize("M, K, N, pad", [(17_000, 32, 256, 0), (20_001, 31, 300, 1), (16_385, 64, 20, 0), (9_000, 125, 130, 3),
                                           (9_001, 128, 40, 0), (8_200, 250, 260, 0), (8_300, 256, 9, 8), (30_000, 1, 70, 0),
                                           (3_000, 1032, 700, 0), (3_001, 1001, 705, 1), (100, 1032, 8_200, 0),
-                                          (129, 1101, 4_100, 0)])
+                                          (129, 1101, 4_100, 0), (9_001, 1101, 2_051, 0), (6_000, 1104, 1_024, 1)])
 @pytest.mark.parametrize("act, bias, p", [("silu", True, 0.0), ("gelu", False, 0.25), ("relu", True, 0.5)])
 def test_gated_many_rows(dtype, M, K, N, pad, act, bias, p):
     """Narrow rows (weights kept in registers, panels of columns, ragged tails of each) and wider ones, at odd and
@@ -352,7 +352,8 @@ def test_int8_extreme_sums():
     assert (got.double() == float(np.float32(128.0 * 128.0 * K))).all()
 
 
-@pytest.mark.parametrize("M, K, N", [(5000, 200, 4100), (5000, 1040, 4100), (5000, 1280, 4100), (100, 4112, 16_400), (1500, 2001, 1700)])
+@pytest.mark.parametrize("M, K, N", [(5000, 200, 4100), (5000, 1040, 4100), (5000, 1280, 4100), (100, 4112, 16_400), (1500, 2001, 1700),
+                                     (3001, 2117, 3203)])
 def test_int8_large_tiles(M, K, N):
     g = gen(12)
     xq = torch.randint(-127, 128, (M, K), generator=g, device=DEV).to(torch.int8)

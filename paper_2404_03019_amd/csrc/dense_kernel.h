@@ -115,22 +115,13 @@ __device__ __forceinline__ void settled(Acc &acc) {
     asm volatile("" : "+a"(acc));
 }
 
-// 16 bytes at p, of which `left` may be read (any number); bytes beyond are 0. What is read ends a run of at
-// least 16 readable bytes, unless `narrow`: a chunk cut short is the run's last 16 bytes, shifted.
+// 16 bytes at p, of which `left` (any number) belong to a run of at least 16 readable bytes; those beyond are to be
+// 0. What is read is at most the run's last 16 bytes, and cut_short shifts them: several loads can so be on
+// their way before the first is waited for. `narrow` runs, of fewer than 16 bytes, are read in elements.
 template <int ES>
 __device__ __forceinline__ chunk_t load_chunk(const char *p, int64_t left, bool narrow) {
+    if (!narrow) return *reinterpret_cast<const chunk_any *>(p + (left < 16 ? left - 16 : 0));
     chunk_t v = {0, 0, 0, 0};
-    if (left >= 16) return *reinterpret_cast<const chunk_any *>(p);
-    if (left <= 0) return v;
-    if (!narrow) {
-        const int cut = 16 - (int)left;   // 1 .. 15 bytes
-        const chunk_t w = *reinterpret_cast<const chunk_any *>(p - cut);
-        const uint64_t lo = (uint64_t)w.y << 32 | w.x, hi = (uint64_t)w.w << 32 | w.z;
-        const int bits = 8 * (cut & 7);
-        const uint64_t carry = bits ? hi << (64 - bits) : 0;
-        const uint64_t a = cut >= 8 ? hi >> bits : lo >> bits | carry, b = cut >= 8 ? 0 : hi >> bits;
-        return chunk_t{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
-    }
     for (int i = 0; i < 16 / ES; ++i) {
         if (i * ES >= left) break;
         uint32_t x;
@@ -145,6 +136,16 @@ __device__ __forceinline__ chunk_t load_chunk(const char *p, int64_t left, bool 
         v.w |= at == 3 ? x : 0;
     }
     return v;
+}
+__device__ __forceinline__ chunk_t cut_short(const chunk_t &w, int64_t left, bool narrow) {
+    if (left >= 16 || narrow) return w;
+    if (left <= 0) return chunk_t{0, 0, 0, 0};
+    const int cut = 16 - (int)left;   // 1 .. 15 bytes
+    const uint64_t lo = (uint64_t)w.y << 32 | w.x, hi = (uint64_t)w.w << 32 | w.z;
+    const int bits = 8 * (cut & 7);
+    const uint64_t carry = bits ? hi << (64 - bits) : 0;
+    const uint64_t a = cut >= 8 ? hi >> bits : lo >> bits | carry, b = cut >= 8 ? 0 : hi >> bits;
+    return chunk_t{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
 }
 
 // One operand's tile of R rows (columns): how its chunks lie in LDS and where they come from. Chunk i
@@ -307,23 +308,27 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
         return Source{basea + (second ? a.seg_a : 0) + sk * inca, (second ? baseb1 : baseb) + sk * incb,
                       DUAL ? baseb1 + sk * incb : nullptr};
     };
-    // Chunk c of the step from `p`, through registers. kleft: how many k there are in the step.
-    auto chunk_a = [&](const Source &p, int c, int64_t kleft) -> chunk_t {
+    // Chunk c of the step from `p`, through registers (`land`: what has been loaded, cut short where it has to
+    // be). kleft: how many k there are in the step; a WHOLE one has all, and one of zeros reads nothing.
+    auto chunk_a = [&](auto WHOLE, bool land, const Source &p, int c, int64_t kleft, chunk_t v) -> chunk_t {
         int64_t row;
         int byte;
         place(TA{}, tid + c * T, mleft, &row, &byte, BM);
-        const int64_t left = KA ? (row < kleft ? mleft * ES - byte : 0) : kleft * ES - byte;
-        return load_chunk<ES>(p.a + row * lda + byte, left, narrow_a);
+        if (!WHOLE && (KA ? row >= kleft : kleft == 0)) return chunk_t{0, 0, 0, 0};
+        const int64_t left = KA ? mleft * ES - byte : WHOLE ? 16 : kleft * ES - byte;
+        return land ? cut_short(v, left, narrow_a) : load_chunk<ES>(p.a + row * lda + byte, left, narrow_a);
     };
-    auto chunk_b = [&](const Source &p, int c, int64_t kleft) -> chunk_t {
+    auto chunk_b = [&](auto WHOLE, bool land, const Source &p, int c, int64_t kleft, chunk_t v) -> chunk_t {
         int64_t row;
         int byte;
         place(TB{}, tid + c * T, nleft, &row, &byte, HB);
-        const int64_t left = KB ? (row < kleft ? nleft * ES - byte : 0) : kleft * ES - byte;
-        return load_chunk<ES>((DUAL && c * T >= HB * 8 ? p.b1 : p.b) + row * ldb + byte, left, narrow_b);
+        if (!WHOLE && (KB ? row >= kleft : kleft == 0)) return chunk_t{0, 0, 0, 0};
+        const int64_t left = KB ? nleft * ES - byte : WHOLE ? 16 : kleft * ES - byte;
+        return land ? cut_short(v, left, narrow_b)
+                    : load_chunk<ES>((DUAL && c * T >= HB * 8 ? p.b1 : p.b) + row * ldb + byte, left, narrow_b);
     };
     // a whole step: straight into LDS, or into registers and from there
-    chunk_t ra[DIRECT ? 1 : CA], rb[DIRECT ? 1 : CB];
+    chunk_t ra[DIRECT ? 1 : CA] = {}, rb[DIRECT ? 1 : CB] = {};
     auto issue = [&](char *lds, int64_t slot) {
         const int64_t s = s0 + slot - odd;
         const bool second = MODE == DENSE_NN && s >= whole;
@@ -339,17 +344,20 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
                                                  (lds_void *)(lds + BM * kStepBytes + (c * T + wave * 64) * 16), 16, 0, 0);
         } else {
 #pragma unroll
-            for (int c = 0; c < CA; ++c) ra[c] = chunk_a(p, c, TA::KS);
+            for (int c = 0; c < CA; ++c) ra[c] = chunk_a(std::true_type(), false, p, c, 0, ra[c]);
 #pragma unroll
-            for (int c = 0; c < CB; ++c) rb[c] = chunk_b(p, c, TA::KS);
+            for (int c = 0; c < CB; ++c) rb[c] = chunk_b(std::true_type(), false, p, c, 0, rb[c]);
         }
     };
     auto land = [&](char *lds) {
         if constexpr (!DIRECT) {
 #pragma unroll
-            for (int c = 0; c < CA; ++c) *reinterpret_cast<chunk_t *>(lds + (tid + c * T) * 16) = ra[c];
+            for (int c = 0; c < CA; ++c)
+                *reinterpret_cast<chunk_t *>(lds + (tid + c * T) * 16) = chunk_a(std::true_type(), true, Source{}, c, 0, ra[c]);
 #pragma unroll
-            for (int c = 0; c < CB; ++c) *reinterpret_cast<chunk_t *>(lds + BM * kStepBytes + (tid + c * T) * 16) = rb[c];
+            for (int c = 0; c < CB; ++c)
+                *reinterpret_cast<chunk_t *>(lds + BM * kStepBytes + (tid + c * T) * 16) =
+                    chunk_b(std::true_type(), true, Source{}, c, 0, rb[c]);
         }
     };
     static_assert(!DUAL || HB * 8 % T == 0, "a thread's chunk is of one column operand");
@@ -396,15 +404,18 @@ __global__ void __launch_bounds__(WM * WN * 64, BM * BN > 128 * 128 ? 1 : 2) den
     auto issue_odd = [&](char *lds, int64_t slot) {
         const Source p = source(MODE == DENSE_NN && slot == 1, whole);
         const int64_t kleft = slot < shorts ? a.K - whole * TA::KS : 0;
-        chunk_t r[CA > CB ? CA : CB];
+        chunk_t r[CA > CB ? CA : CB] = {};
 #pragma unroll
-        for (int c = 0; c < CA; ++c) r[c] = chunk_a(p, c, kleft);
+        for (int c = 0; c < CA; ++c) r[c] = chunk_a(std::false_type(), false, p, c, kleft, r[c]);
 #pragma unroll
-        for (int c = 0; c < CA; ++c) *reinterpret_cast<chunk_t *>(lds + (tid + c * T) * 16) = r[c];
+        for (int c = 0; c < CA; ++c)
+            *reinterpret_cast<chunk_t *>(lds + (tid + c * T) * 16) = chunk_a(std::false_type(), true, p, c, kleft, r[c]);
 #pragma unroll
-        for (int c = 0; c < CB; ++c) r[c] = chunk_b(p, c, kleft);
+        for (int c = 0; c < CB; ++c) r[c] = chunk_b(std::false_type(), false, p, c, kleft, r[c]);
 #pragma unroll
-        for (int c = 0; c < CB; ++c) *reinterpret_cast<chunk_t *>(lds + BM * kStepBytes + (tid + c * T) * 16) = r[c];
+        for (int c = 0; c < CB; ++c)
+            *reinterpret_cast<chunk_t *>(lds + BM * kStepBytes + (tid + c * T) * 16) =
+                chunk_b(std::false_type(), true, p, c, kleft, r[c]);
     };
 #pragma unroll 1
     for (int j = 0; j < 2; ++j) {

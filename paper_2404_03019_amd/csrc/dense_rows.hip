@@ -181,6 +181,7 @@ __global__ void __launch_bounds__(kRowsBlock) join_kernel(const DenseArgs a) {
         Columns<4> c;
         load_columns<E, EPI, 4>(a, n, c);
         float y[4];
+        if constexpr (EPI == DENSE_I8) y[0] = a.sx[m];
         if constexpr (EPI == DENSE_GATED)
             with_act(a.act, [&](auto act) {
                 finish<E, EPI, decltype(act)::value, 4, DUAL>(a, 0, m, n, m * a.ldo + n, c, g, u, y);

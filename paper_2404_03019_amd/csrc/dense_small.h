@@ -50,6 +50,25 @@ __global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
 
+    // What the thread finishes at the end. The 8-bit product's scales and bias, cold, are loaded first (one row, 4,096
+    // -> 4,096 11.0 -> 10.5 us); 16-bit ones would be waited for here, to be widened.
+    constexpr bool FIRST = EPI == DENSE_I8;
+    constexpr int R = (kUnits + kSmallWaves * 64 - 1) / (kSmallWaves * 64);
+    Columns<4> cols[R];
+    float ys[R][4];
+    auto ahead = [&](int r) {
+        const int unit = tid + r * kSmallWaves * 64, i = unit / (PF * 64), j = unit / 64 % PF;
+        const int64_t m = m0 + 16 * i + r16, n = n0 + 16 * j + 4 * c4;
+        if (unit >= kUnits || m >= a.M || n >= a.N) return;
+        load_columns<E, EPI, 4>(a, n, cols[r]);
+        if constexpr (EPI == DENSE_GATED_BWD) load_wide<E, 4>(a.grad, m * a.ldg + n, a.N - n, ys[r]);
+        if constexpr (EPI == DENSE_I8) ys[r][0] = a.sx[m];
+    };
+    if constexpr (FIRST) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) ahead(r);
+    }
+
     const int64_t kbytes = a.K * ES, whole = kbytes / 64;
     const bool narrow = kbytes < 16;
     // C of the wave's steps from s, all loaded before the first is multiplied. With MASK steps from `whole`
@@ -79,9 +98,9 @@ __global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs
     typedef std::integral_constant<int, U / 2> Half;
     // the step that K cuts short is the wave's whose turn it is; its loads go first
     const bool mine = whole % kSmallWaves == wave && whole * 64 < kbytes;
+    const int64_t left = kbytes - whole * 64 - c4 * 16;
     chunk_t xs[FM], ws[FN];
     if (mine) {
-        const int64_t left = kbytes - whole * 64 - c4 * 16;
 #pragma unroll
         for (int j = 0; j < FN; ++j) ws[j] = load_chunk<ES>(pw[j] + whole * 64, left, narrow);
 #pragma unroll
@@ -93,6 +112,10 @@ __global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs
     else if (s < whole) steps(Half(), std::true_type(), s);
     if (mine) {
 #pragma unroll
+        for (int j = 0; j < FN; ++j) ws[j] = cut_short(ws[j], left, narrow);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) xs[i] = cut_short(xs[i], left, narrow);
+#pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = mma<E>(ws[j], xs[i], acc[i][j]);
@@ -103,7 +126,10 @@ __global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs
 #pragma unroll
         for (int j = 0; j < FN; ++j) part[wave][i * FN + j][lane] = acc[i][j];
     __syncthreads();
-    for (int unit = tid; unit < kUnits; unit += kSmallWaves * 64) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int unit = tid + r * kSmallWaves * 64;
+        if (unit >= kUnits) break;
         const int i = unit / (PF * 64), j = unit / 64 % PF;
         Acc vg = part[0][i * FN + j][lane], vu = Acc{0, 0, 0, 0};
         if constexpr (DUAL) vu = part[0][i * FN + PF + j][lane];
@@ -121,14 +147,13 @@ __global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs
             u[v] = vu[v];
         }
         if (in) {
-            Columns<4> c;
-            load_columns<E, EPI, 4>(a, n, c);
-            float y[4];
-            if constexpr (EPI == DENSE_GATED_BWD) load_wide<E, 4>(a.grad, m * a.ldg + n, a.N - n, y);
+            if constexpr (!FIRST) ahead(r);
             if constexpr (EPI == DENSE_GATED || EPI == DENSE_GATED_BWD)
-                with_act(a.act, [&](auto act) { finish<E, EPI, decltype(act)::value, 4, DUAL>(a, 0, m, n, m * a.ldo + n, c, g, u, y); });
+                with_act(a.act, [&](auto act) {
+                    finish<E, EPI, decltype(act)::value, 4, DUAL>(a, 0, m, n, m * a.ldo + n, cols[r], g, u, ys[r]);
+                });
             else
-                finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, m * a.ldo + n, c, g, u, y);
+                finish<E, EPI, ACT_NONE, 4, DUAL>(a, 0, m, n, m * a.ldo + n, cols[r], g, u, ys[r]);
         }
         if constexpr (EPI == DENSE_GATED_BWD) {   // a row of column sums for each 16 rows
             float sg[4], su[4];

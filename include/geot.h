@@ -468,8 +468,11 @@ geot_status_t geot_transpose_edges(const int64_t *col, int64_t num_x_rows, const
  *    its columns; any element-aligned address will do. Biases and scales are contiguous.
  *  - Sums, activations and scales are held in fp32 (int32 for 8-bit products); every
  *    output is rounded once, to nearest even, to its type.
- *  - The temporary memory of a call is the stream's buffer up to 64 MB, else, and under
- *    capture, stream-ordered allocations of the library's pool. All calls can be captured
+ *  - Addresses and row strides that are multiples of 16 bytes are read fastest; large 16-
+ *    and 8-bit products over others may copy their operands into such rows first.
+ *  - The temporary memory of a call (partial sums, such copies, and what is named below)
+ *    is the stream's buffer up to 64 MB, else, and under capture, stream-ordered
+ *    allocations of the library's pool. All calls can be captured
  *    in a HIP graph. Results do not depend on timing.
  *  - Row strides, sizes, types and overlaps are checked on the host
  *    (GEOT_ERROR_INVALID_VALUE). Zero rows or output columns are a no-op; a product over
@@ -506,8 +509,9 @@ typedef enum {
  *   w_gate, w_up  [out_features x in_features], one row stride for both
  *   b_gate, b_up  [out_features] or NULL (zero), each
  *   out           [rows x out_features], overwritten; must not overlap an input
- * All of `type`. g, u and their product are never written to memory (few rows over a long in_features
- * are summed in parts: fp32 partial sums in the temporary memory).         */
+ * All of `type`. g, u and their product are never written to memory (where there are few outputs over a long
+ * in_features they are summed in parts: fp32 partial sums in the temporary memory).
+ * exp in the sigmoid and (16-bit) in GELU is good to about (1 + |g|) 2^-23 of its value. */
 geot_status_t geot_gated_linear(const void *x, geot_dtype_t type, int64_t rows, int64_t in_features, int64_t x_stride,
                                 const void *w_gate, const void *w_up, int64_t out_features, int64_t w_stride,
                                 const void *b_gate, const void *b_up, geot_activation_t act, double p, uint64_t seed,
@@ -521,8 +525,7 @@ geot_status_t geot_gated_linear(const void *x, geot_dtype_t type, int64_t rows, 
  *   grad_b_gate, grad_b_up: the column sums of dG and dU   [out_features]
  * grad_x, the two grad_w together, and each grad_b may be NULL (skipped). Outputs are contiguous, of
  * `type`, overwritten, and overlap nothing. dG and dU are rounded to `type` between the
- * passes (the bias gradients sum them before that). Temporary memory: dG and dU, and one copy of the weights
- * for grad_x.                                                               */
+ * passes (the bias gradients sum them before that). Temporary memory: dG and dU. */
 geot_status_t geot_gated_linear_backward(const void *grad_out, int64_t grad_stride, const void *x, geot_dtype_t type,
                                          int64_t rows, int64_t in_features, int64_t x_stride, const void *w_gate,
                                          const void *w_up, int64_t out_features, int64_t w_stride, const void *b_gate,

@@ -73,23 +73,49 @@ __global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs
 
     const int64_t kbytes = a.K * ES, whole = kbytes / 64;
     const bool narrow = kbytes < 16;
+    // 16-byte loads at addresses that are no multiple of 4 take several times as long. Where there are such rows
+    // (UNEVEN) the five words that hold a chunk are loaded instead, and shifted; each holds a byte of it. fp16, 722 rows,
+    // 769 -> 693 44 -> 22 us (768 -> 693 18), 64 rows, 769 -> 2,731 17.6 -> 9.8; 8-bit, 722 rows 25 -> 15.
+    const bool uneven = ES < 4 && (((uintptr_t)a.a | (uintptr_t)a.b0 | (DUAL ? (uintptr_t)a.b1 : 0) | (uintptr_t)(a.lda * ES) |
+                                    (uintptr_t)(a.ldb * ES)) & 3) != 0;
     // C of the wave's steps from s, all loaded before the first is multiplied. With MASK steps from `whole`
     // on do not exist: the last one is loaded in their place and not multiplied.
-    auto steps = [&](auto count, auto mask, int64_t s) {
+    auto steps = [&](auto count, auto mask, auto words, int64_t s) {
         constexpr int C = decltype(count)::value;
-        constexpr bool MASK = decltype(mask)::value;
+        constexpr bool MASK = decltype(mask)::value, UNEVEN = decltype(words)::value;
         chunk_t x[C][FM], w[C][FN];
+        uint32_t xe[C][FM], we[C][FN];
+        auto load = [&](const char *p, int64_t at, chunk_t *v, uint32_t *e) {
+            const uint32_t off = UNEVEN ? (uint32_t)(uintptr_t)p & 3 : 0;
+            const char *q = p - off + at;
+            *v = *reinterpret_cast<const chunk_any *>(q);
+            if constexpr (UNEVEN) *e = *reinterpret_cast<const uint32_t *>(q + (off ? 16 : 12));
+        };
+        auto shift = [&](const char *p, chunk_t *v, uint32_t e) {
+            const uint32_t off = (uint32_t)(uintptr_t)p & 3;
+            const chunk_t t = *v;
+            v->x = __builtin_amdgcn_alignbyte(t.y, t.x, off);
+            v->y = __builtin_amdgcn_alignbyte(t.z, t.y, off);
+            v->z = __builtin_amdgcn_alignbyte(t.w, t.z, off);
+            v->w = off ? __builtin_amdgcn_alignbyte(e, t.w, off) : t.w;
+        };
 #pragma unroll
         for (int u = 0; u < C; ++u) {
             const int64_t st = s + kSmallWaves * u, at = (MASK && st >= whole ? whole - 1 : st) * 64;
 #pragma unroll
-            for (int j = 0; j < FN; ++j) w[u][j] = *reinterpret_cast<const chunk_any *>(pw[j] + at);
+            for (int j = 0; j < FN; ++j) load(pw[j], at, &w[u][j], &we[u][j]);
 #pragma unroll
-            for (int i = 0; i < FM; ++i) x[u][i] = *reinterpret_cast<const chunk_any *>(px[i] + at);
+            for (int i = 0; i < FM; ++i) load(px[i], at, &x[u][i], &xe[u][i]);
         }
 #pragma unroll
         for (int u = 0; u < C; ++u) {
             if (MASK && s + kSmallWaves * u >= whole) break;
+            if constexpr (UNEVEN) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j) shift(pw[j], &w[u][j], we[u][j]);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) shift(px[i], &x[u][i], xe[u][i]);
+            }
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -98,6 +124,7 @@ __global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs
     };
     typedef std::integral_constant<int, U> Full;
     typedef std::integral_constant<int, U / 2> Half;
+    typedef std::integral_constant<int, !DUAL && FM + FN == 8 ? 1 : U / 2> Few;   // (more would not fit the registers)
     // the step that K cuts short is the wave's whose turn it is; its loads go first
     const bool mine = whole % kSmallWaves == wave && whole * 64 < kbytes;
     const int64_t left = kbytes - whole * 64 - c4 * 16;
@@ -109,9 +136,13 @@ __global__ void __launch_bounds__(kSmallWaves * 64) small_kernel(const DenseArgs
         for (int i = 0; i < FM; ++i) xs[i] = load_chunk<ES>(px[i] + whole * 64, left, narrow);
     }
     int64_t s = wave;
-    for (; s + kSmallWaves * (U - 1) < whole; s += kSmallWaves * U) steps(Full(), std::false_type(), s);
-    if (s + kSmallWaves * (U / 2) < whole) steps(Full(), std::true_type(), s);
-    else if (s < whole) steps(Half(), std::true_type(), s);
+    if constexpr (ES < 4) {
+        if (uneven)
+            for (; s < whole; s += kSmallWaves * Few::value) steps(Few(), std::true_type(), std::true_type(), s);
+    }
+    for (; s + kSmallWaves * (U - 1) < whole; s += kSmallWaves * U) steps(Full(), std::false_type(), std::false_type(), s);
+    if (s + kSmallWaves * (U / 2) < whole) steps(Full(), std::true_type(), std::false_type(), s);
+    else if (s < whole) steps(Half(), std::true_type(), std::false_type(), s);
     if (mine) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) ws[j] = cut_short(ws[j], left, narrow);

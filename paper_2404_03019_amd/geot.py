@@ -757,16 +757,13 @@ def gated_linear_backward(grad_out: torch.Tensor, x: torch.Tensor, w_gate: torch
 def quantize_rows(x: torch.Tensor):
     """(q, scale): the rows of x in 8 bits, scale[r] * q[r] = x[r] to half a step (geot_quantize_rows).
 
-    x [rows, F] fp32, bf16 or fp16; q int8 [rows, F] (its rows start on 16 bytes: where F is no multiple of 16 it
-    is a slice of a wider tensor), scale fp32 [rows]. A row that holds NaN or an infinity
-    gets scale NaN."""
+    x [rows, F] fp32, bf16 or fp16; q int8 [rows, F], its rows a multiple of 16 bytes apart (so it is contiguous
+    where F is one), scale fp32 [rows]. A row that holds NaN or an infinity gets scale NaN."""
     ld = _rows(x, "x", _FLOATS)
     _on_gpu(x=x)
     R, F = x.shape
     ldq = F + -F % 16 or 1   # rows on 16 bytes: what the product loads fastest
-    q = torch.empty((R, ldq), dtype=torch.int8, device=x.device)
-    if ldq != F:
-        q = q[:, :F]
+    q = torch.empty_strided((R, F), (ldq, 1), dtype=torch.int8, device=x.device)
     scale = torch.empty(R, dtype=torch.float32, device=x.device)
     _launch(lib().geot_quantize_rows, x.get_device(), x.data_ptr(), DTYPES[x.dtype], R, F, ld, q.data_ptr(), ldq,
             scale.data_ptr())

@@ -196,6 +196,40 @@ def test_gated_many_rows(dtype, M, K, N, pad, act, bias, p):
             ref.check(t, *w, f"gradient {i}")
 
 
+@pytest.mark.parametrize("dtype", (BF16, F16))
+@pytest.mark.parametrize("M, K, N, pad", [(700, 769, 693, 0), (1000, 1001, 900, 1), (300, 2051, 400, 3), (64, 770, 2731, 1),
+                                          (30, 333, 700, 0), (5, 1003, 4100, 2), (1, 41, 9, 1)])
+def test_gated_at_odd_addresses(dtype, M, K, N, pad):
+    """Few rows or tiles over rows that start at any even address, alone and as a slice that starts at its second
+    element, with NaN around it."""
+    g = gen(M + K + N)
+    wide = torch.full((M + 2 * N, K + pad + 1), math.nan, dtype=dtype, device=DEV)
+    wide[:, 1:K + 1] = rand(g, M + 2 * N, K, dtype=dtype) / K ** 0.25
+    x, wg, wu = (t[:, 1:K + 1] for t in (wide[:M], wide[M:M + N], wide[M + N:]))
+    bg, bu, grad = rand(g, N, dtype=dtype), rand(g, N, dtype=dtype), rand(g, M, N, dtype=dtype)
+    want = ref.gated64(x, wg, wu, bg, bu, "silu", None, grad)
+    ref.check(geot.gated_linear(x, wg, wu, bg, bu), *want[0], "out")
+    for i, (t, w) in enumerate(zip(geot.gated_linear_backward(grad, x, wg, wu, bg, bu), want[1:])):
+        ref.check(t, *w, f"gradient {i}")
+    cx, cg, cu = (t.contiguous() for t in (x, wg, wu))
+    ref.check(geot.gated_linear(cx, cg, cu, bg, bu), *want[0], "out of whole tensors")
+
+
+@pytest.mark.parametrize("M, K, N", [(700, 769, 693), (1000, 1001, 900), (1000, 1002, 900), (300, 2051, 400), (64, 770, 2731),
+                                     (20, 333, 700), (5, 1003, 4100), (1, 41, 9)])
+@pytest.mark.parametrize("at", [0, 1, 2, 3])
+def test_int8_at_odd_addresses(M, K, N, at):
+    g = gen(M * K + N)
+    buf = torch.randint(-128, 128, ((M + N) * (K + 1) + at,), generator=g, device=DEV).to(torch.int8)
+    both = buf[at:].view(M + N, K + 1)[:, :K]
+    xq, wq = both[:M], both[M:]
+    one_m, one_n = torch.ones(M, device=DEV), torch.ones(N, device=DEV)
+    got = geot.linear_int8(xq, one_m, wq, one_n, dtype=F32)
+    # sums below 2^24 in magnitude 2^14 K are not exact in fp32 beyond 1024 columns: half a last bit
+    want = xq.double() @ wq.double().t()
+    ref.check(got, want, torch.zeros_like(want), "out")
+
+
 def test_gated_gradient_against_differences():
     """fp32 gradients against central differences of the block in 64 bits (whose error is of the order of h^2)."""
     M, K, N, h = 5, 9, 6, 1e-4
